@@ -383,6 +383,102 @@ typedef struct smile_backward_io {
 smile_status smile_layer_backward(smile_ctx *ctx, const smile_backward_io *io, float dloss,
                                   void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators in 8 bits around and inside the layer: the norm in front of it, products of 8-bit operands,
+ * and activations kept in 8 bits for the backward pass.  They need no ctx (but smile_fp8_dispatch), allocate
+ * nothing and take tensors of any size within the stated limits.
+ *
+ * 8-bit rows.  A row of K values is cut into blocks of 128 (the last one may be shorter).  A block has a
+ * power-of-two scale 2^(b - 127), kept as its byte b, and each value a code in 8-bit floating point (1 sign,
+ * 4 exponent, 3 fraction bits, bias 7, no infinity, NaN = 0x7f / 0xff): value = code * 2^(b - 127).
+ *   codes  [N][C][smile_fp8_pitch(K)]        bytes; columns K .. pitch - 1 are zero codes
+ *   scales [N][ceil(K/128)][smile_fp8_scale_pitch(C)] bytes; entry r of a block's line belongs to row r
+ * Packing: b is the least byte >= 1 for which the block's largest magnitude is at most 448 * 2^(b - 127), so
+ * a block of zeros has b = 1; value / 2^(b - 127) is rounded to the nearest code, ties to even, with
+ * gradual underflow.  Infinities and NaN become NaN codes and do not count for b.
+ * 8-bit weights w[N][Nout][K] have one scale for each 128 x 128 block:
+ *   codes  [N][Nout][smile_fp8_pitch(K)],  scales [N][ceil(K/128)][smile_fp8_scale_pitch(ceil(Nout/128))]
+ * and in transposed form the same codes as [N][K][smile_fp8_pitch(Nout)] with scales
+ * [N][ceil(Nout/128)][smile_fp8_scale_pitch(ceil(K/128))].
+ * Why powers of two: the matrix cores apply them for nothing, scaling rounds nothing, and the values
+ * are exact in bfloat16 (and in half precision within its range).
+ *
+ * `rows`: int32 [N] on the device, valid rows of each group (clamped to 0 .. C), or NULL for all C.  Rows at
+ * or beyond it are neither read nor written.
+ * Limits: N, C, T, K, Nout, d >= 1; K, Nout, d % 8 == 0; N <= 4096; K, Nout <= 32768, d of the norm <= 16384; N*C, N*Nout and
+ * T <= 2^30; elements of any tensor below 2^40.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of a row of codes (K up to a multiple of 128) and of a line of scales (rows up to a multiple of 16).  Host helpers. */
+int32_t smile_fp8_pitch(int32_t K);
+int32_t smile_fp8_scale_pitch(int32_t rows);
+
+/* Root-mean-square norm with the residual's addition, over the d columns of T rows in storage type `dtype`:
+ *   s[t,:] = x[t,:] + residual[t,:], rounded to the storage type (residual NULL: s = x)
+ *   rstd[t] = (mean_k s[t,k]^2 + eps)^(-1/2);   y[t,k] = s[t,k] * rstd[t] * weight[k]
+ * from s as it is rounded, in fp32.  Outputs, each of which may be NULL, but not both y and y8: sum (s; NULL without
+ * residual), y in the storage type, y8 with y8_scale (8-bit rows, N = 1, C = T; rounded from fp32, not from y), rstd [T].
+ * weight[d] in the storage type; eps > 0.  sum may be x or residual itself, y may be x. */
+smile_status smile_rms_norm(int32_t T, int32_t d, int32_t dtype, const void *x, const void *residual, const void *weight,
+                            float eps, void *sum, void *y, void *y8, void *y8_scale, float *rstd, void *stream);
+
+/* Its gradients.  s and rstd as smile_rms_norm gave them, dy the gradient of y, dsum that of s from its other uses (NULL: none):
+ *   u = s * rstd, g = weight * dy:   ds = dsum + rstd * (g - u * mean_k(g * u)),   dweight[k] = sum_t dy[t,k] * u[t,k]
+ * ds (of x and of residual alike) in the storage type; ds may be dy or dsum itself.  dweight fp32 [d], summed in a fixed order.
+ * The 8-bit output counts as y itself.  workspace: at least
+ * smile_rms_norm_backward_workspace_bytes bytes, 256-byte aligned. */
+smile_status smile_rms_norm_backward_workspace_bytes(int32_t T, int32_t d, size_t *bytes);
+smile_status smile_rms_norm_backward(int32_t T, int32_t d, int32_t dtype, const void *dy, const void *dsum, const void *s,
+                                     const void *weight, const float *rstd, void *ds, float *dweight, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
+/* src[N][C][K] in `dtype` to 8-bit rows, and 8-bit rows to dst[N][C][K] in `dtype` (in half precision what
+ * is beyond +-65504 becomes that). */
+smile_status smile_fp8_pack_rows(int32_t N, int32_t C, int32_t K, int32_t dtype, const void *src, const int32_t *rows,
+                                 void *codes, void *scales, void *stream);
+smile_status smile_fp8_unpack_rows(int32_t N, int32_t C, int32_t K, int32_t dtype, const void *codes, const void *scales,
+                                   const int32_t *rows, void *dst, void *stream);
+
+/* w[N][Nout][K] in `dtype` to 8-bit weights, and to their transposed form where codes_t and scales_t are given (both or neither). */
+smile_status smile_fp8_pack_weights(int32_t N, int32_t Nout, int32_t K, int32_t dtype, const void *w, void *codes, void *scales,
+                                    void *codes_t, void *scales_t, void *stream);
+
+/* smile_dispatch for 8-bit rows of the tokens (N = 1, C = T, K = d_model): row t of x8 and its scales to row slot[t] of its
+ * expert's buffer in xe8 [N][C][...], xe_scale.  Any dtype of the ctx. */
+smile_status smile_fp8_dispatch(smile_ctx *ctx, const void *x8, const void *x_scale, const int32_t *group_idx,
+                                const int32_t *local_idx, const int32_t *slot, void *xe8, void *xe_scale, void *stream);
+
+enum { SMILE_ACT_NONE = 2 };   /* smile_fp8_gemm: no activation */
+
+/* Grouped product of 8-bit rows with 8-bit weights, rows r < rows[e] of every group e:
+ *   p[r,o] = sum_k x[e,r,k] * w[e,o,k] + bias[e,o]           (fp32)
+ *   v = act(p), or, where grad8 is given, p * act'(g) with g the value that grad8 keeps of the pre-activation
+ * y: v in the storage type; y8 / y_scale: v as 8-bit rows; pre8 / pre_scale: p as 8-bit rows, the checkpoint that a
+ * backward product takes as grad8.  With weights in transposed form it is the gradient of the rows.
+ * GELU is the erf form with the accuracy of the 16-bit expert FFN. */
+typedef struct smile_fp8_gemm_args {
+    int32_t N, C, K, Nout;       /* groups, rows of each group's buffer, contraction length, columns of the result */
+    int32_t dtype, act;          /* storage type of y and bias; SMILE_ACT_* */
+    const void *x8, *x_scale;    /* 8-bit rows [N][C][K] */
+    const void *w8, *w_scale;    /* 8-bit weights [N][Nout][K] */
+    const void *bias;            /* [N][Nout] or NULL; not with grad8 */
+    const int32_t *rows;         /* [N] or NULL */
+    void *y;                     /* [N][C][Nout] or NULL */
+    void *y8, *y_scale;          /* 8-bit rows [N][C][Nout], or both NULL; y or y8 is given */
+    void *pre8, *pre_scale;      /* 8-bit rows [N][C][Nout], or both NULL; not with grad8 */
+    const void *grad8, *grad_scale;   /* 8-bit rows [N][C][Nout], or both NULL; needs an activation */
+} smile_fp8_gemm_args;
+smile_status smile_fp8_gemm(const smile_fp8_gemm_args *args, void *stream);
+
+/* Weight gradient from an operand kept in 8 bits: dw[e,o,k] = sum_{r < rows[e]} dy[e,r,o] * x[e,r,k], dy[N][C][Nout] and
+ * dw[N][Nout][K] in `dtype`, x8 / x_scale 8-bit rows [N][C][K].  Products of 16-bit values (K and Nout % 64 == 0) or of fp32 ones,
+ * summed in fp32 and rounded once; a group without rows gets zeros.  workspace: at least smile_fp8_weight_grad_workspace_bytes
+ * bytes, 256-byte aligned (the operand in `dtype`). */
+smile_status smile_fp8_weight_grad_workspace_bytes(int32_t N, int32_t C, int32_t K, int32_t dtype, size_t *bytes);
+smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K, int32_t dtype, const void *dy, const void *x8,
+                                   const void *x_scale, const int32_t *rows, void *dw, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+
 #ifdef __cplusplus
 }
 #endif

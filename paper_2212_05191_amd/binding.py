@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libsmile.so")
 _lib = None
 
 DTYPE = {"f32": 0, "bf16": 1, "f16": 2}
-ACT = {"relu": 0, "gelu": 1}
+ACT = {"relu": 0, "gelu": 1, "none": 2}   # "none": products of 8-bit operands only
 
 OK, INVALID_ARG, BAD_SHAPE, UNSUPPORTED, WORKSPACE, HIP_ERROR = range(6)
 
@@ -48,6 +48,11 @@ class BackwardIO(C.Structure):
         "dye", "dgate", "dlp", "dlq", "dxe", "dx", "dw_inter", "dw_intra", "dw1", "dw2")]
 
 
+class Fp8GemmArgs(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("N", "C", "K", "Nout", "dtype", "act")] + [(k, C.c_void_p) for k in (
+        "x8", "x_scale", "w8", "w_scale", "bias", "rows", "y", "y8", "y_scale", "pre8", "pre_scale", "grad8", "grad_scale")]
+
+
 EXPORTS = (
     "smile_status_string", "smile_version", "smile_capacity", "smile_validate_desc", "smile_workspace_bytes",
     "smile_create", "smile_create_with_workspace", "smile_destroy", "smile_gate_logits", "smile_route_bilevel",
@@ -55,6 +60,9 @@ EXPORTS = (
     "smile_dispatch", "smile_dispatch_hop1", "smile_dispatch_hop2", "smile_expert_ffn", "smile_expert_ffn_up", "smile_expert_ffn_down", "smile_expert_ffn_up_timed", "smile_combine", "smile_aux_loss", "smile_layer_forward",
     "smile_backward_workspace_bytes", "smile_combine_backward", "smile_route_backward", "smile_expert_ffn_backward",
     "smile_dispatch_backward", "smile_gate_weights_backward", "smile_layer_backward",
+    "smile_fp8_pitch", "smile_fp8_scale_pitch", "smile_rms_norm", "smile_rms_norm_backward_workspace_bytes",
+    "smile_rms_norm_backward", "smile_fp8_pack_rows", "smile_fp8_unpack_rows", "smile_fp8_pack_weights",
+    "smile_fp8_dispatch", "smile_fp8_gemm", "smile_fp8_weight_grad_workspace_bytes", "smile_fp8_weight_grad",
 )
 
 
@@ -102,6 +110,19 @@ def load() -> C.CDLL:
     lib.smile_dispatch_backward.argtypes = [vp] * 11
     lib.smile_gate_weights_backward.argtypes = [vp] * 7 + [C.c_size_t, vp]
     lib.smile_layer_backward.argtypes = [vp, C.POINTER(BackwardIO), C.c_float, vp, C.c_size_t, vp]
+    sz = C.POINTER(C.c_size_t)
+    lib.smile_fp8_pitch.argtypes = [i32]
+    lib.smile_fp8_scale_pitch.argtypes = [i32]
+    lib.smile_rms_norm.argtypes = [i32] * 3 + [vp] * 3 + [C.c_float] + [vp] * 6
+    lib.smile_rms_norm_backward_workspace_bytes.argtypes = [i32, i32, sz]
+    lib.smile_rms_norm_backward.argtypes = [i32] * 3 + [vp] * 8 + [C.c_size_t, vp]
+    lib.smile_fp8_pack_rows.argtypes = [i32] * 4 + [vp] * 5
+    lib.smile_fp8_unpack_rows.argtypes = [i32] * 4 + [vp] * 5
+    lib.smile_fp8_pack_weights.argtypes = [i32] * 4 + [vp] * 6
+    lib.smile_fp8_dispatch.argtypes = [vp] * 9
+    lib.smile_fp8_gemm.argtypes = [C.POINTER(Fp8GemmArgs), vp]
+    lib.smile_fp8_weight_grad_workspace_bytes.argtypes = [i32] * 4 + [sz]
+    lib.smile_fp8_weight_grad.argtypes = [i32] * 5 + [vp] * 6 + [C.c_size_t, vp]
     for name in EXPORTS[3:]:
         getattr(lib, name).restype = i32
     lib.smile_kernel_timing_name.restype = C.c_char_p
@@ -360,6 +381,202 @@ def make_backward_io(x, w_inter, w_intra, w1, w2, fwd: "LayerBuffers", dy, bwd: 
     for k, v in bwd.__dict__.items():
         setattr(io, k, _ptr(v))
     return io
+
+
+# ------------------------------------------------------------------ operators in 8 bits
+
+def _dtype_code(t) -> int:
+    """DTYPE code of a torch tensor's element type."""
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"storage type {t.dtype} is none of float32, bfloat16, float16")
+    return code
+
+
+def smile_fp8_pitch(K: int) -> int:
+    return int(load().smile_fp8_pitch(int(K)))
+
+
+def smile_fp8_scale_pitch(rows: int) -> int:
+    return int(load().smile_fp8_scale_pitch(int(rows)))
+
+
+def _has_shape(name, t, shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+
+
+def _check_rows8(name, codes, scales, N, rows, K):
+    """8-bit rows [N][rows][K]: the shapes that the library takes for granted."""
+    _has_shape(name, codes, (N, rows, smile_fp8_pitch(K)))
+    _has_shape(name + " scales", scales, (N, smile_fp8_pitch(K) // 128, smile_fp8_scale_pitch(rows)))
+
+
+def _check_weights8(name, codes, scales, N, Nout, K):
+    _has_shape(name, codes, (N, Nout, smile_fp8_pitch(K)))
+    _has_shape(name + " scales", scales, (N, smile_fp8_pitch(K) // 128, smile_fp8_scale_pitch(-(-Nout // 128))))
+
+
+def _check_dtype(name, t, code):
+    if t is not None and _dtype_code(t) != code:
+        raise TypeError(f"{name} is {t.dtype}, of another storage type than the rest")
+
+
+def _check_f32(name, t):
+    if t is not None and _dtype_code(t) != 0:
+        raise TypeError(f"{name} is {t.dtype}, not float32")
+
+
+def _check_counts(rows, N):
+    import torch
+    if rows is not None and rows.dtype != torch.int32:
+        raise TypeError(f"rows is {rows.dtype}, not int32")
+    _has_shape("rows", rows, (N,))
+
+
+def alloc_fp8_rows(N, rows, K, device="cuda:0"):
+    """Codes and scales of 8-bit rows [N][rows][K], zeroed."""
+    import torch
+    pitch = smile_fp8_pitch(K)
+    return (torch.zeros((N, rows, pitch), dtype=torch.uint8, device=device),
+            torch.zeros((N, pitch // 128, smile_fp8_scale_pitch(rows)), dtype=torch.uint8, device=device))
+
+
+def alloc_fp8_weights(N, Nout, K, device="cuda:0"):
+    """Codes and scales of 8-bit weights [N][Nout][K], zeroed."""
+    import torch
+    pitch = smile_fp8_pitch(K)
+    return (torch.zeros((N, Nout, pitch), dtype=torch.uint8, device=device),
+            torch.zeros((N, pitch // 128, smile_fp8_scale_pitch(-(-Nout // 128))), dtype=torch.uint8, device=device))
+
+
+def smile_rms_norm(x, residual, weight, eps, sum=None, y=None, y8=None, y8_scale=None, rstd=None, stream=None):
+    """x[T, d] (+ residual, or None) -> sum, y, 8-bit y, rstd: whichever are given."""
+    T, d = x.shape
+    code = _dtype_code(x)
+    for name, t, shape in (("residual", residual, (T, d)), ("weight", weight, (d,)), ("sum", sum, (T, d)), ("y", y, (T, d))):
+        _has_shape(name, t, shape)
+        _check_dtype(name, t, code)
+    _has_shape("rstd", rstd, (T,))
+    _check_f32("rstd", rstd)
+    if y8 is not None:
+        _check_rows8("y8", y8, y8_scale, 1, T, d)
+    _check(load().smile_rms_norm(T, d, code, _ptr(x), _ptr(residual), _ptr(weight), float(eps), _ptr(sum), _ptr(y), _ptr(y8),
+                                 _ptr(y8_scale), _ptr(rstd), _stream(stream)), "smile_rms_norm")
+
+
+def smile_rms_norm_backward_workspace_bytes(T, d) -> int:
+    out = C.c_size_t(0)
+    _check(load().smile_rms_norm_backward_workspace_bytes(int(T), int(d), C.byref(out)), "smile_rms_norm_backward_workspace_bytes")
+    return int(out.value)
+
+
+def smile_rms_norm_backward(dy, s, weight, rstd, ds, dweight, workspace, dsum=None, stream=None):
+    T, d = dy.shape
+    code = _dtype_code(dy)
+    for name, t, shape in (("s", s, (T, d)), ("weight", weight, (d,)), ("ds", ds, (T, d)), ("dsum", dsum, (T, d))):
+        _has_shape(name, t, shape)
+        _check_dtype(name, t, code)
+    for name, t, shape in (("rstd", rstd, (T,)), ("dweight", dweight, (d,))):
+        _has_shape(name, t, shape)
+        _check_f32(name, t)
+    _check(load().smile_rms_norm_backward(T, d, code, _ptr(dy), _ptr(dsum), _ptr(s), _ptr(weight), _ptr(rstd), _ptr(ds),
+                                          _ptr(dweight), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                          _stream(stream)), "smile_rms_norm_backward")
+
+
+def _grouped(t):
+    """(N, C, K) of a tensor [N, C, K] or [C, K]"""
+    return tuple(t.shape) if t.dim() == 3 else (1, *t.shape)
+
+
+def smile_fp8_pack_rows(src, codes, scales, rows=None, stream=None):
+    """src[N, C, K] (or [C, K]) to 8-bit rows; only the first rows[e] of each group."""
+    N, cap, K = _grouped(src)
+    _check_rows8("codes", codes, scales, N, cap, K)
+    _check_counts(rows, N)
+    _check(load().smile_fp8_pack_rows(N, cap, K, _dtype_code(src), _ptr(src), _ptr(rows), _ptr(codes), _ptr(scales),
+                                      _stream(stream)), "smile_fp8_pack_rows")
+
+
+def smile_fp8_unpack_rows(codes, scales, dst, rows=None, stream=None):
+    """8-bit rows to dst[N, C, K] (or [C, K])."""
+    N, cap, K = _grouped(dst)
+    _check_rows8("codes", codes, scales, N, cap, K)
+    _check_counts(rows, N)
+    _check(load().smile_fp8_unpack_rows(N, cap, K, _dtype_code(dst), _ptr(codes), _ptr(scales), _ptr(rows), _ptr(dst),
+                                        _stream(stream)), "smile_fp8_unpack_rows")
+
+
+def smile_fp8_pack_weights(w, codes, scales, codes_t=None, scales_t=None, stream=None):
+    """w[N, Nout, K] (or [Nout, K]) to 8-bit weights, and to their transposed form."""
+    N, Nout, K = _grouped(w)
+    _check_weights8("codes", codes, scales, N, Nout, K)
+    if codes_t is not None:
+        _check_weights8("codes_t", codes_t, scales_t, N, K, Nout)
+    _check(load().smile_fp8_pack_weights(N, Nout, K, _dtype_code(w), _ptr(w), _ptr(codes), _ptr(scales), _ptr(codes_t),
+                                         _ptr(scales_t), _stream(stream)), "smile_fp8_pack_weights")
+
+
+def smile_fp8_dispatch(ctx: Ctx, x8, x_scale, group_idx, local_idx, slot, xe8, xe_scale, stream=None):
+    d = ctx.desc
+    _check_rows8("x8", x8, x_scale, 1, d.T, d.d_model)
+    _check_rows8("xe8", xe8, xe_scale, d.n_groups * d.m_local, d.capacity, d.d_model)
+    _check(load().smile_fp8_dispatch(ctx.handle, _ptr(x8), _ptr(x_scale), _ptr(group_idx), _ptr(local_idx), _ptr(slot), _ptr(xe8),
+                                     _ptr(xe_scale), _stream(stream)), "smile_fp8_dispatch")
+
+
+def make_fp8_gemm_args(x8, x_scale, w8, w_scale, K, Nout, rows=None, act="none", bias=None, y=None, y8=None, y_scale=None,
+                       pre8=None, pre_scale=None, grad8=None, grad_scale=None, dtype=None) -> Fp8GemmArgs:
+    """The argument block of smile_fp8_gemm; dtype is that of y and bias, and needed only where neither is given.  The block
+    keeps the tensors alive."""
+    N, cap = x8.shape[:2]
+    _check_rows8("x8", x8, x_scale, N, cap, K)
+    _check_weights8("w8", w8, w_scale, N, Nout, K)
+    for name, codes, scales in (("y8", y8, y_scale), ("pre8", pre8, pre_scale), ("grad8", grad8, grad_scale)):
+        if codes is not None:
+            _check_rows8(name, codes, scales, N, cap, Nout)
+    if y is not None and _grouped(y) != (N, cap, Nout):
+        raise ValueError(f"y has shape {tuple(y.shape)}, not {(N, cap, Nout)}")
+    if bias is not None and bias.numel() != N * Nout:
+        raise ValueError(f"bias has shape {tuple(bias.shape)}, not {(N, Nout)}")
+    _check_counts(rows, N)
+    code = _dtype_code(y) if y is not None else _dtype_code(bias) if bias is not None else DTYPE[dtype or "bf16"]
+    _check_dtype("bias", bias, code)
+    args = Fp8GemmArgs(N, cap, int(K), int(Nout), code, ACT[act])
+    tensors = dict(x8=x8, x_scale=x_scale, w8=w8, w_scale=w_scale, bias=bias, rows=rows, y=y, y8=y8, y_scale=y_scale, pre8=pre8,
+                   pre_scale=pre_scale, grad8=grad8, grad_scale=grad_scale)
+    for k, v in tensors.items():
+        setattr(args, k, _ptr(v))
+    args.tensors = tensors
+    return args
+
+
+def smile_fp8_gemm(args: Fp8GemmArgs, stream=None):
+    _check(load().smile_fp8_gemm(C.byref(args), _stream(stream)), "smile_fp8_gemm")
+
+
+def smile_fp8_weight_grad_workspace_bytes(N, cap, K, dtype) -> int:
+    out = C.c_size_t(0)
+    code = DTYPE[dtype] if isinstance(dtype, str) else int(dtype)
+    _check(load().smile_fp8_weight_grad_workspace_bytes(int(N), int(cap), int(K), code, C.byref(out)),
+           "smile_fp8_weight_grad_workspace_bytes")
+    return int(out.value)
+
+
+def smile_fp8_weight_grad(dy, x8, x_scale, dw, workspace, rows=None, stream=None):
+    """dw[N, Nout, K] = dy[N, C, Nout]^T . (8-bit rows [N, C, K]) over the first rows[e] rows of each group."""
+    N, cap, Nout = _grouped(dy)
+    K = dw.shape[-1]
+    if _grouped(dw) != (N, Nout, K):
+        raise ValueError(f"dw has shape {tuple(dw.shape)}, not {(N, Nout, K)}")
+    _check_rows8("x8", x8, x_scale, N, cap, K)
+    _check_dtype("dw", dw, _dtype_code(dy))
+    _check_counts(rows, N)
+    _check(load().smile_fp8_weight_grad(N, cap, Nout, K, _dtype_code(dy), _ptr(dy), _ptr(x8), _ptr(x_scale), _ptr(rows), _ptr(dw),
+                                        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "smile_fp8_weight_grad")
 
 
 # ------------------------------------------------------------------ device buffers for one layer

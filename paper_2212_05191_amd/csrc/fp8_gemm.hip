@@ -1,0 +1,185 @@
+// Grouped product of 8-bit rows with 8-bit weights:  p[e][r][o] = sum_k x[e][r][k] w[e][o][k] + bias, with the activation, its derivative at a
+// kept pre-activation, and 8-bit outputs in the epilogue.
+//
+// fp8_gemm_rows_kernel, for few rows a group: what counts is the weights' way from HBM and the latency of a tile, so a tile is 32 rows x 32 WN
+// columns, the contraction is split over WK waves, and every wave reads both operands straight into the registers of its matrix
+// instructions, four blocks of 128 ahead: a lane holds row (or column) lane % 32 and the half lane / 32 of its 128 bytes.  The order of
+// the k inside a block does not matter as long as both operands have the same.  The waves' sums meet in LDS in a fixed order, and the
+// epilogue works on runs of eight columns, sixteen lanes to a block of the 8-bit outputs.
+#include "fp8_device.hpp"
+#include "fp8_internal.hpp"
+
+namespace smile {
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// D(o, r) += sum over 64 k of W(o, k) X(r, k) with a scale for each lane's row; e4m3 both (format 0), scales in byte 0
+__device__ __forceinline__ f32x16 mfma_scaled(u32x4 w0, u32x4 w1, u32x4 x0, u32x4 x1, f32x16 c, uint32_t sw, uint32_t sx)
+{
+    const i32x8 w = {(int)w0[0], (int)w0[1], (int)w0[2], (int)w0[3], (int)w1[0], (int)w1[1], (int)w1[2], (int)w1[3]};
+    const i32x8 x = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, (int)sw, 0, (int)sx);
+}
+
+// Eight neighbouring elements in the storage type `dtype`, which is the same for the whole launch
+__device__ __forceinline__ void load8(int dtype, const void *base, size_t at, float *v)
+{
+    if (dtype == SMILE_DTYPE_BF16) Piece<SMILE_DTYPE_BF16>::widen(Piece<SMILE_DTYPE_BF16>::load(base, at), v);
+    else if (dtype == SMILE_DTYPE_F16) Piece<SMILE_DTYPE_F16>::widen(Piece<SMILE_DTYPE_F16>::load(base, at), v);
+    else Piece<SMILE_DTYPE_F32>::widen(Piece<SMILE_DTYPE_F32>::load(base, at), v);
+}
+__device__ __forceinline__ void store8(int dtype, void *base, size_t at, const float *v)
+{
+    if (dtype == SMILE_DTYPE_BF16) Piece<SMILE_DTYPE_BF16>::store(base, at, Piece<SMILE_DTYPE_BF16>::narrow(v));
+    else if (dtype == SMILE_DTYPE_F16) Piece<SMILE_DTYPE_F16>::store(base, at, Piece<SMILE_DTYPE_F16>::narrow(v));
+    else Piece<SMILE_DTYPE_F32>::store(base, at, Piece<SMILE_DTYPE_F32>::narrow(v));
+}
+__device__ __forceinline__ void activate8(int act, float *v)
+{
+    if (act == 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate<1>(v[k]);
+    } else if (act == 3) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate<3>(v[k]);
+    }
+}
+
+// The epilogue of eight columns col .. col + 7 of row r of group e; ROWS8: sixteen lanes of a DPP row hold a whole block of 128 columns.
+// Columns beyond Nout are zero codes and no elements.
+template <bool ROWS8>
+__device__ __forceinline__ void finish8(const Fp8Gemm &a, int e, int r, int col, float *v)
+{
+    const size_t row = (size_t)e * a.C + r;
+    const int NB = (a.Nout + kFp8Block - 1) / kFp8Block;
+    const size_t code = row * ((size_t)NB * kFp8Block) + col, scale = ((size_t)e * NB + col / kFp8Block) * a.Cs + r;
+    const bool in = col < a.Nout;
+    if (!in) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    } else if (a.bias) {
+        float b[8];
+        load8(a.dtype, a.bias, (size_t)e * a.Nout + col, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += b[k];
+    }
+    if constexpr (ROWS8) {
+        if (a.p8) {
+            u32x2 c;
+            const uint32_t byte = pack_block(v, c);
+            *reinterpret_cast<u32x2 *>(a.p8 + code) = c;
+            if (col % kFp8Block == 0) a.ps[scale] = (uint8_t)byte;
+        }
+        if (a.g8) {
+            const u32x2 c = *reinterpret_cast<const u32x2 *>(a.g8 + code);
+            const float s = scale_value(a.gs[scale]);
+            float g[8];
+            unpack4(c[0], s, g);
+            unpack4(c[1], s, g + 4);
+            if (a.act == 1) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= activate_grad<1>(g[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= activate_grad<2>(g[k]);
+            }
+        } else {
+            activate8(a.act, v);
+        }
+        if (a.y8) {
+            u32x2 c;
+            const uint32_t byte = pack_block(v, c);
+            *reinterpret_cast<u32x2 *>(a.y8 + code) = c;
+            if (col % kFp8Block == 0) a.ys[scale] = (uint8_t)byte;
+        }
+    } else {
+        activate8(a.act, v);
+    }
+    if (a.y && in) store8(a.dtype, a.y, row * a.Nout + col, v);
+}
+
+// WN waves side by side, 32 columns each; WK waves share the contraction
+template <int WN, int WK, bool ROWS8>
+__global__ __launch_bounds__(64 * WN * WK) void fp8_gemm_rows_kernel(Fp8Gemm a)
+{
+    constexpr int BN = 32 * WN, PITCH = BN + 4, THREADS = 64 * WN * WK, AHEAD = 4;
+    static_assert(!ROWS8 || BN == kFp8Block, "a tile is one block of the 8-bit outputs");
+    __shared__ __attribute__((aligned(16))) float sums[WK * 32 * PITCH];
+    int tile = blockIdx.x;
+    const int rt = tile % a.row_tiles;
+    tile /= a.row_tiles;
+    const int ct = tile % a.col_tiles, e = tile / a.col_tiles;
+    const int valid = rows_of(a.rows, e, a.C);
+    if (rt * 32 >= valid) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wn = wave % WN, wk = wave / WN;
+    const int half = lane >> 5, K = a.KB * kFp8Block;
+    const int row = min(rt * 32 + (lane & 31), valid - 1), col = min(ct * BN + wn * 32 + (lane & 31), a.Nout - 1);   // beyond: the last one again
+    const uint8_t *x = a.x + ((size_t)e * a.C + row) * K + half * 64, *w = a.w + ((size_t)e * a.Nout + col) * K + half * 64;
+    const uint8_t *xs = a.xs + (size_t)e * a.KB * a.Cs + row, *ws = a.ws + (size_t)e * a.KB * a.Ws + col / kFp8Block;
+    struct Block {
+        u32x4 x[4], w[4];
+        uint8_t xs, ws;
+    } block[AHEAD];
+    const auto request = [&](Block &b, int kb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b.w[i] = *reinterpret_cast<const u32x4 *>(w + (size_t)kb * kFp8Block + 16 * i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b.x[i] = *reinterpret_cast<const u32x4 *>(x + (size_t)kb * kFp8Block + 16 * i);
+        b.ws = ws[(size_t)kb * a.Ws], b.xs = xs[(size_t)kb * a.Cs];
+    };
+    f32x16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+    const int kb0 = a.KB * wk / WK, kb1 = a.KB * (wk + 1) / WK;
+    for_constants<AHEAD>([&](auto i) {
+        if (kb0 + decltype(i)::value < kb1) request(block[decltype(i)::value], kb0 + decltype(i)::value);
+    });
+    for (int kb = kb0; kb < kb1; kb += AHEAD) {
+        for_constants<AHEAD>([&](auto i) {
+            constexpr int I = decltype(i)::value;
+            if (kb + I >= kb1) return;
+            Block &b = block[I];
+            acc = mfma_scaled(b.w[0], b.w[1], b.x[0], b.x[1], acc, b.ws, b.xs);
+            acc = mfma_scaled(b.w[2], b.w[3], b.x[2], b.x[3], acc, b.ws, b.xs);
+            if (kb + I + AHEAD < kb1) request(b, kb + I + AHEAD);
+        });
+    }
+    // element v of a lane: column 8 (v / 4) + 4 half + v % 4 of row lane % 32
+    float *mine = sums + (wk * 32 + (lane & 31)) * PITCH + wn * 32 + 4 * half;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4 *>(mine + 8 * q) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    for (int p = threadIdx.x; p < 32 * BN / 8; p += THREADS) {
+        const int lr = p / (BN / 8), lc = p % (BN / 8) * 8, r = rt * 32 + lr, c = ct * BN + lc;
+        if (r >= valid || (!ROWS8 && c >= a.Nout)) continue;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < WK; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += sums[(k * 32 + lr) * PITCH + lc + j];
+        finish8<ROWS8>(a, e, r, c, v);
+    }
+}
+
+template <int WN, int WK, bool ROWS8>
+hipError_t launch_rows(Fp8Gemm a, hipStream_t s)
+{
+    a.row_tiles = (a.C + 31) / 32;
+    a.col_tiles = (a.Nout + 32 * WN - 1) / (32 * WN);
+    const long long tiles = (long long)a.N * a.row_tiles * a.col_tiles;
+    if (tiles >= 1ll << 31) return hipErrorInvalidValue;
+    SMILE_LAUNCH((fp8_gemm_rows_kernel<WN, WK, ROWS8>), dim3((unsigned)tiles), dim3(64 * WN * WK), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &, hipStream_t s)
+{
+    if (g.y8 || g.p8 || g.g8) return launch_rows<4, 2, true>(g, s);
+    return launch_rows<1, 4, false>(g, s);
+}
+
+}  // namespace smile

@@ -4,7 +4,7 @@
 #include <cstdlib>
 #include <new>
 
-#include "smile_internal.hpp"
+#include "api_checks.hpp"
 
 namespace smile {
 
@@ -28,8 +28,6 @@ struct TimerScope {
         if (mine) tls_kernel_timer = nullptr;
     }
 };
-
-static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 Layout workspace_layout(const smile_layer_desc &d)
 {
@@ -60,20 +58,6 @@ void place_routing(Workspace &ws, const Layout &L, char *base)
     ws.block_q_sum = reinterpret_cast<float *>(base + L.off_block_q_sum);
     ws.rank_in_block = reinterpret_cast<int32_t *>(base + L.off_rank_in_block);
     ws.pos_in_block = reinterpret_cast<int32_t *>(base + L.off_pos_in_block);
-}
-
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// required pointer: non-NULL and 16-byte aligned
-static bool bad(const void *p) { return p == nullptr || !aligned16(p); }
-// optional pointer: NULL or 16-byte aligned
-static bool bad_opt(const void *p) { return p != nullptr && !aligned16(p); }
-
-static smile_status from_hip(hipError_t e)
-{
-    if (e == hipSuccess) return SMILE_OK;
-    (void)hipGetLastError();   // do not leave a sticky launch error behind for the caller's next call
-    return SMILE_HIP_ERROR;
 }
 
 }  // namespace smile

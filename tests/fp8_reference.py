@@ -1,0 +1,129 @@
+"""The 8-bit operators in 64 bits, written from their definition in include/smile.h with numpy alone."""
+import math
+
+import numpy as np
+
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}    # half a step, relative to the value
+TINY = {"f32": 2.0 ** -149, "bf16": 2.0 ** -133, "f16": 2.0 ** -25}   # half a step of the subnormals (fp32: one)
+
+
+def up(v, q):
+    return -(-v // q) * q
+
+
+def code_values():
+    """What the 256 codes stand for (NaN at 0x7f and 0xff)."""
+    out = np.empty(256)
+    for c in range(256):
+        sign, e, f = (-1.0 if c & 0x80 else 1.0), (c >> 3) & 15, c & 7
+        out[c] = math.nan if (c & 0x7f) == 0x7f else sign * (f * 2.0 ** -9 if e == 0 else (1 + f / 8) * 2.0 ** (e - 7))
+    return out
+
+
+CODES = code_values()
+
+
+def encode(u):
+    """Nearest codes of |u| <= 448, ties to the even code; NaN for what is not finite."""
+    u = np.asarray(u, np.float64)
+    a = np.abs(u)
+    fine = np.isfinite(u)
+    positive = CODES[:0x7f]                                   # ascending, 0 .. 448
+    x = np.where(fine, a, 0.0)
+    hi = np.clip(np.searchsorted(positive, x), 1, 0x7e)
+    lo = hi - 1
+    d_lo, d_hi = x - positive[lo], positive[hi] - x
+    code = np.where((d_lo < d_hi) | ((d_lo == d_hi) & (lo % 2 == 0)), lo, hi)
+    code = np.where(fine, code, 0x7f)
+    return (code + np.where(np.signbit(u), 0x80, 0)).astype(np.uint8)
+
+
+def scale_bytes(largest):
+    """The least byte >= 1 with largest <= 448 * 2^(byte - 127)."""
+    largest = np.asarray(largest, np.float64)
+    b = np.ones(largest.shape, np.int64)
+    for k in range(2, 255):
+        b = np.where(largest > 448.0 * 2.0 ** (k - 1 - 127), k, b)
+    return b
+
+
+def _finite_max(a, axis):
+    return np.max(np.where(np.isfinite(a), np.abs(a), 0.0), axis=axis)
+
+
+def pack_rows(v):
+    """v[N, C, K] -> codes[N, C, pitch], scales[N, blocks, pitch of C] (entries of no row: 0)."""
+    N, C, K = v.shape
+    P, B = up(K, 128), up(K, 128) // 128
+    a = np.zeros((N, C, P))
+    a[:, :, :K] = v
+    a = a.reshape(N, C, B, 128)
+    b = scale_bytes(_finite_max(a, 3))
+    with np.errstate(invalid="ignore"):
+        codes = encode(a / 2.0 ** (b[..., None] - 127.0)).reshape(N, C, P)
+    scales = np.zeros((N, B, up(C, 16)), np.uint8)
+    scales[:, :, :C] = b.transpose(0, 2, 1)
+    return codes, scales
+
+
+def pack_weights(w):
+    N, O, K = w.shape
+    NB, B = up(O, 128) // 128, up(K, 128) // 128
+    a = np.zeros((N, NB * 128, B * 128))
+    a[:, :O, :K] = w
+    a = a.reshape(N, NB, 128, B, 128)
+    b = scale_bytes(_finite_max(a, (2, 4)))
+    with np.errstate(invalid="ignore"):
+        codes = encode(a / 2.0 ** (b[:, :, None, :, None] - 127.0)).reshape(N, NB * 128, B * 128)[:, :O]
+    scales = np.zeros((N, B, up(NB, 16)), np.uint8)
+    scales[:, :, :NB] = b.transpose(0, 2, 1)
+    return codes, scales
+
+
+def unpack_rows(codes, scales, K):
+    N, C, P = codes.shape
+    s = 2.0 ** (scales[:, :, :C].astype(np.float64).transpose(0, 2, 1) - 127.0)
+    return (CODES[codes].reshape(N, C, P // 128, 128) * s[..., None]).reshape(N, C, P)[:, :, :K]
+
+
+def unpack_weights(codes, scales, K):
+    N, O, P = codes.shape
+    s = 2.0 ** (scales.astype(np.float64).transpose(0, 2, 1) - 127.0)
+    return (CODES[codes].reshape(N, O, P // 128, 128) * np.repeat(s, 128, axis=1)[:, :O, :, None]).reshape(N, O, P)[:, :, :K]
+
+
+def row_step(v, scales):
+    """Half the distance of the codes at each value of 8-bit rows v[N, C, K] with these scales."""
+    N, C, K = v.shape
+    s = np.repeat(2.0 ** (scales[:, :, :C].astype(np.float64).transpose(0, 2, 1) - 127.0), 128, axis=2)[:, :, :K]
+    e = np.floor(np.log2(np.maximum(np.abs(v) / s, 2.0 ** -6)))
+    return s * 2.0 ** (e - 4)
+
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
+
+
+def act(v, name):
+    if name == "none":
+        return v
+    return np.maximum(v, 0.0) if name == "relu" else v * 0.5 * _erfc(-v / math.sqrt(2.0))
+
+
+def act_grad(v, name):
+    if name == "relu":
+        return (v > 0).astype(np.float64)
+    return 0.5 * _erfc(-v / math.sqrt(2.0)) + v * np.exp(-0.5 * v * v) / math.sqrt(2.0 * math.pi)
+
+
+def rms_norm(s, weight, eps):
+    rstd = 1.0 / np.sqrt(np.mean(s * s, axis=1) + eps)
+    return rstd, s * rstd[:, None] * weight
+
+
+def rms_norm_backward(dy, s, weight, eps, dsum):
+    rstd = 1.0 / np.sqrt(np.mean(s * s, axis=1) + eps)
+    u = s * rstd[:, None]
+    g = dy * weight
+    ds = rstd[:, None] * (g - u * np.mean(g * u, axis=1)[:, None])
+    return ds + (0.0 if dsum is None else dsum), np.sum(dy * u, axis=0)
