@@ -1,27 +1,16 @@
 // Grouped product of 8-bit rows with 8-bit weights:  p[e][r][o] = sum_k x[e][r][k] w[e][o][k] + bias, with the activation, its derivative at a
 // kept pre-activation, and 8-bit outputs in the epilogue.
 //
-// fp8_gemm_rows_kernel, for few rows a group: what counts is the weights' way from HBM and the latency of a tile, so a tile is 32 rows x 32 WN
+// Two kernels.  fp8_gemm_ring.hpp has the one for many rows.  fp8_gemm_rows_kernel, for few rows a group: what counts is the weights' way from HBM and the latency of a tile, so a tile is 32 rows x 32 WN
 // columns, the contraction is split over WK waves, and every wave reads both operands straight into the registers of its matrix
 // instructions, four blocks of 128 ahead: a lane holds row (or column) lane % 32 and the half lane / 32 of its 128 bytes.  The order of
 // the k inside a block does not matter as long as both operands have the same.  The waves' sums meet in LDS in a fixed order, and the
 // epilogue works on runs of eight columns, sixteen lanes to a block of the 8-bit outputs.
-#include "fp8_device.hpp"
-#include "fp8_internal.hpp"
+#include "fp8_gemm_ring.hpp"
 
 namespace smile {
 
 namespace {
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-// D(o, r) += sum over 64 k of W(o, k) X(r, k) with a scale for each lane's row; e4m3 both (format 0), scales in byte 0
-__device__ __forceinline__ f32x16 mfma_scaled(u32x4 w0, u32x4 w1, u32x4 x0, u32x4 x1, f32x16 c, uint32_t sw, uint32_t sx)
-{
-    const i32x8 w = {(int)w0[0], (int)w0[1], (int)w0[2], (int)w0[3], (int)w1[0], (int)w1[1], (int)w1[2], (int)w1[3]};
-    const i32x8 x = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, (int)sw, 0, (int)sx);
-}
 
 // Eight neighbouring elements in the storage type `dtype`, which is the same for the whole launch
 __device__ __forceinline__ void load8(int dtype, const void *base, size_t at, float *v)
@@ -141,8 +130,8 @@ __global__ __launch_bounds__(64 * WN * WK) void fp8_gemm_rows_kernel(Fp8Gemm a)
             constexpr int I = decltype(i)::value;
             if (kb + I >= kb1) return;
             Block &b = block[I];
-            acc = mfma_scaled(b.w[0], b.w[1], b.x[0], b.x[1], acc, b.ws, b.xs);
-            acc = mfma_scaled(b.w[2], b.w[3], b.x[2], b.x[3], acc, b.ws, b.xs);
+            acc = mfma_scaled(set_high(set_low(b.w[0]), b.w[1]), set_high(set_low(b.x[0]), b.x[1]), acc, b.ws, b.xs);
+            acc = mfma_scaled(set_high(set_low(b.w[2]), b.w[3]), set_high(set_low(b.x[2]), b.x[3]), acc, b.ws, b.xs);
             if (kb + I + AHEAD < kb1) request(b, kb + I + AHEAD);
         });
     }
@@ -176,10 +165,15 @@ hipError_t launch_rows(Fp8Gemm a, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &, hipStream_t s)
+hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s)
 {
-    if (g.y8 || g.p8 || g.g8) return launch_rows<4, 2, true>(g, s);
-    return launch_rows<1, 4, false>(g, s);
+    const bool rows8 = g.y8 || g.p8 || g.g8;
+    if (g.C <= 64) return rows8 ? launch_rows<4, 2, true>(g, s) : launch_rows<1, 4, false>(g, s);
+    // 128 x 128, two on a CU; 128 x 256 moves a third less through L2, which counts where there are many rounds of long contractions and no 8-bit
+    // epilogue for the other workgroup to hide (us: 8192 x 8192 x 8192 656 -> 468, 64 groups x 256 rows, 1024 -> 4096 143 -> 157)
+    const long long wide = (long long)g.N * ((g.C + 127) / 128) * ((g.Nout + 255) / 256);
+    if (!rows8 && wide >= 6ll * tune.cus) return launch_fp8_ring<1, 1, 2, 2, 1, false>(g, tune, s);
+    return rows8 ? launch_fp8_ring<1, 1, 1, 1, 2, true>(g, tune, s) : launch_fp8_ring<1, 1, 1, 1, 2, false>(g, tune, s);
 }
 
 }  // namespace smile

@@ -50,6 +50,7 @@ struct Fp8Gemm {
     int Cs, Ws;                      // bytes of a line of scales: rows, blocks of columns
     int dtype, act;                  // act: 0 none, 1 ReLU, 3 GELU
     int row_tiles, col_tiles;
+    bool backwards;                  // ring kernels: walk the tiles from the last group to the first
 };
 hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s);
 
