@@ -19,28 +19,28 @@ inline int fp8_scale_pitch(int rows) { return (rows + 15) / 16 * 16; }
 
 namespace {
 
-// |v| as bits, 0 for infinities and NaN: what counts for a block's scale.  Ordered like the magnitudes.
-__device__ __forceinline__ uint32_t magnitude(float v)
-{
-    const uint32_t a = __float_as_uint(v) & 0x7fffffffu;
-    return a < 0x7f800000u ? a : 0u;
-}
+// What counts for a block's scale, ordered like the magnitudes of finite values: 2 |v| as bits, plus one exponent, so that infinities and NaN wrap
+// below 2^24 and every finite value is at or above it (one instruction, and half of another for the maximum of two)
+__device__ __forceinline__ uint32_t magnitude_key(float v) { return (__float_as_uint(v) << 1) + 0x01000000u; }
+__device__ __forceinline__ uint32_t magnitude_of(uint32_t key) { return (max(key, 0x01000000u) - 0x01000000u) >> 1; }
 
-// The scale's byte for a block's largest magnitude m 2^p: 2^(p-8) if m <= 1.75 (448 = 1.75 * 2^8), else 2^(p-7).  At least 1, so
-// that the reciprocal is finite; at most 247.
+// The scale's byte for a block's largest magnitude m 2^p (as bits): 2^(p-8) if m <= 1.75 (448 = 1.75 * 2^8), else 2^(p-7).  At least 1, the
+// smallest normal power; at most 247.
 __device__ __forceinline__ uint32_t scale_byte(uint32_t largest)
 {
     const uint32_t p = (largest + 0x1fffffu) >> 23;   // a fraction beyond .75 carries into the exponent
     return max(p, 9u) - 8u;
 }
-__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }              // byte >= 1
-__device__ __forceinline__ float scale_reciprocal(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }   // byte >= 1
 
-// Four values times `r` as codes, rounded to nearest even
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d, float r)
+// Four values over a scale (a power of two) as codes, rounded to nearest even: the instruction divides as it converts
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d, float scale)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * r, b * r, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * r, d * r, w, true);
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true);
+    return __builtin_bit_cast(uint32_t, w);
 }
 __device__ __forceinline__ void unpack4(uint32_t w, float s, float *v)
 {
@@ -130,9 +130,9 @@ __device__ __forceinline__ uint32_t pack_block(const float *v, u32x2 &codes)
 {
     uint32_t largest = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) largest = max(largest, magnitude(v[k]));
-    const uint32_t byte = scale_byte(max_of_16(largest));
-    const float r = scale_reciprocal(byte);
+    for (int k = 0; k < 8; ++k) largest = max(largest, magnitude_key(v[k]));
+    const uint32_t byte = scale_byte(magnitude_of(max_of_16(largest)));
+    const float r = scale_value(byte);
     codes[0] = pack4(v[0], v[1], v[2], v[3], r), codes[1] = pack4(v[4], v[5], v[6], v[7], r);
     return byte;
 }

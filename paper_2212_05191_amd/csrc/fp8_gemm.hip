@@ -6,6 +6,8 @@
 // instructions, four blocks of 128 ahead: a lane holds row (or column) lane % 32 and the half lane / 32 of its 128 bytes.  The order of
 // the k inside a block does not matter as long as both operands have the same.  The waves' sums meet in LDS in a fixed order, and the
 // epilogue works on runs of eight columns, sixteen lanes to a block of the 8-bit outputs.
+#include <algorithm>
+
 #include "fp8_gemm_ring.hpp"
 
 namespace smile {
@@ -165,15 +167,28 @@ hipError_t launch_rows(Fp8Gemm a, hipStream_t s)
 
 }  // namespace
 
+// Which kernel and tile.  us of a kernel, 32-row tiles first:
+//   * y alone: 32 x 32 tiles with the contraction split over four waves while they are at most two a CU.  1 group x 16 rows, 1024 -> 4096 (128 tiles) 4.8 and
+//     7.6, 128 rows (512) 7.1 and 8.1; 4096 -> 1024 9.5 and 15.8; 16 x 16, 3072 -> 768 (384) 12.8 and 13.0; beyond, 16 x 48 (768) 20.5 and
+//     13.0, 16 x 1, 768 -> 3072 (1536) 11.9 and 9.8, 8 x 128, 256 -> 1024 (1024) 6.5 and 5.5.
+//   * 8-bit rows, whose 128 columns a workgroup of eight waves needs: contractions of four blocks or less and at most one tile a CU.  4 x 16,
+//     512 -> 1024 6.8 and 7.6, 8 x 128, 256 -> 1024 6.0 and 7.7; but 1 x 16, 1024 -> 4096 9.8 and 9.0, 16 x 1, 768 -> 3072 13.0 and 11.8.
+//   * else 128 x 128, two on a CU; 128 x 256, which moves a quarter less through L2, for long contractions without an epilogue that the other workgroup
+//     would hide, where there are four rounds of such tiles: 8192 x 8192 x 8192 498 -> 462, 128 groups x 256 rows, 3072 -> 768 119 -> 113; 64 x
+//     256, 4096 -> 1024 (three rounds) 98 -> 104, 16384 x 1024 -> 4096 81 -> 92.
 hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s)
 {
     const bool rows8 = g.y8 || g.p8 || g.g8;
-    if (g.C <= 64) return rows8 ? launch_rows<4, 2, true>(g, s) : launch_rows<1, 4, false>(g, s);
-    // 128 x 128, two on a CU; 128 x 256 moves a third less through L2, which counts where there are many rounds of long contractions and no 8-bit
-    // epilogue for the other workgroup to hide (us: 8192 x 8192 x 8192 656 -> 468, 64 groups x 256 rows, 1024 -> 4096 143 -> 157)
-    const long long wide = (long long)g.N * ((g.C + 127) / 128) * ((g.Nout + 255) / 256);
-    if (!rows8 && wide >= 6ll * tune.cus) return launch_fp8_ring<1, 1, 2, 2, 1, false>(g, tune, s);
-    return rows8 ? launch_fp8_ring<1, 1, 1, 1, 2, true>(g, tune, s) : launch_fp8_ring<1, 1, 1, 1, 2, false>(g, tune, s);
+    const auto tiles = [&](int rows, int columns) {
+        return (long long)g.N * ((g.C + rows - 1) / rows) * ((g.Nout + columns - 1) / columns);
+    };
+    // (the ring kernels' scale offsets are 32 bits)
+    if ((long long)g.KB * std::max(g.Cs, g.Ws) >= 1ll << 31 || (rows8 ? g.KB <= 4 && tiles(32, 128) <= tune.cus : tiles(32, 32) <= 2 * tune.cus))
+        return rows8 ? launch_rows<4, 2, true>(g, s) : launch_rows<1, 4, false>(g, s);
+    if (g.g8) return launch_fp8_ring<1, 2, kFp8Slope>(g, tune, s);
+    if (rows8) return launch_fp8_ring<1, 2, kFp8Rows>(g, tune, s);
+    if (g.act == 0 && g.KB >= 16 && tiles(128, 256) >= 4 * tune.cus) return launch_fp8_ring<2, 1, kFp8Y>(g, tune, s);
+    return launch_fp8_ring<1, 2, kFp8Y>(g, tune, s);
 }
 
 }  // namespace smile

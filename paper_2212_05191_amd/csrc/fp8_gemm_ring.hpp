@@ -4,9 +4,13 @@
 //   * the scales of a slab travel with its unit A0: every wave loads one line of 256 bytes, wave 0 those of the tile's rows, wave 1 the word
 //     that holds those of its column blocks; they lie behind the stage's operands in LDS;
 //   * a lane reads its rows' bytes together with A0 and hands them to the instruction, which multiplies them in.
-// What bounds it: per slab a 256 x 256 tile moves 64 KB through L2 for 2048 matrix cycles, 32 bytes a cycle and CU, about what L2 delivers; 128 x
-// 128 moves 64 bytes a cycle, but two workgroups share a CU and the epilogue of one runs beside the contraction of the other.
-// GELU with its 8-bit output takes nearly two vector-ALU cycles an output, as long as 2048 k of contraction.
+// What bounds it: the latency of the units, 2 us under load, against 7 of 8 slots in flight (112 KB a CU with two workgroups, 84 KB with one of 128 x
+// 256), and the epilogue, which adds to it: 64 groups x 256 rows, 1024 -> 4096, GELU and 8-bit rows: 81 us without an epilogue, 118 without its
+// stores, 131 in all (1.05 PFLOP/s; the weights' way from HBM is 52).  Per slab 128 x 128 moves 64 KB through L2 for 1024 matrix
+// cycles of a CU, two workgroups side by side; 8192 x 8192 x 8192 2.2 PFLOP/s (2.4 in tiles of 128 x 256; a library product 2.9, at the 1.6 GHz
+// that the power limit leaves).  Tried and taken back: the epilogue in slices beside the next tile's phases from a second set of accumulators
+// (no gain: one wave issues a vector instruction every 5.5 cycles), 256 x 256 tiles (spill), requests into L2 a tile ahead (slower).
+// GELU with its 8-bit output takes 25 vector instructions an output.
 //
 // The 8-bit epilogue needs the largest magnitude of a row in a block of 128 columns, which two waves share (and, in tiles of 128 columns,
 // both parts of each): the waves exchange theirs through LDS.
@@ -21,10 +25,13 @@ namespace smile {
 
 namespace {
 
-// QA0, QA1 / QB0, QB1: 32-wide blocks per wave in the units A0, A1 / B0, B1.  ROWS8: the epilogue with 8-bit rows in or out.
-template <int QA0, int QA1, int QB0, int QB1, int OCC, bool ROWS8>
+enum { kFp8Y, kFp8Rows, kFp8Slope };   // y alone; 8-bit rows too; both times the activation's derivative at kept 8-bit rows
+
+// QA0, QA1 / QB0, QB1: 32-wide blocks per wave in the units A0, A1 / B0, B1.  KIND: what the epilogue does.
+template <int QA0, int QA1, int QB0, int QB1, int OCC, int KIND>
 __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
 {
+#ifdef __HIP_DEVICE_COMPILE__   // (the host has no type for a buffer resource)
     constexpr int NW = 4, BM = 64 * (QA0 + QA1), BN = 64 * (QB0 + QB1), TM = QA0 + QA1, TN = QB0 + QB1, CB = BN / kFp8Block;
     enum { A0, B0, B1, A1 };                                            // units of a slab, in the order of the ring
     constexpr int kExt[4] = {64 * QA0, 64 * QB0, 64 * QB1, 64 * QA1};   // rows (columns) of a unit
@@ -36,7 +43,7 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
     constexpr int GPW = 2 * (TM + TN), SCALES = (BM + BN) * 128, STAGE = SCALES + NW * 256;
     constexpr int QB = QB0;                                       // both parts of a tile's columns are as wide
     constexpr int SROW = QB * 64 + 16;                            // bytes of a staged row
-    constexpr int STAGING = NW * 32 * SROW, LARGEST = ROWS8 ? 2 * CB * BM * 4 : 0;   // one exchange of magnitudes: [wn][block][row]
+    constexpr int STAGING = NW * 32 * SROW, LARGEST = KIND != kFp8Y ? 2 * CB * BM * 4 : 0;   // one exchange of magnitudes: [wn][block][row]
     static_assert(QB0 == QB1 && (CB == 1 || CB == 2) && BN == CB * kFp8Block && QA0 >= 1 && QA1 >= 1 && QA0 <= 2 && QA1 <= 2, "tile shapes");
     static_assert((2 * STAGE + STAGING + 2 * LARGEST) * OCC <= kLdsPerCu, "LDS");
     __shared__ __attribute__((aligned(16))) char ring_lds[2 * STAGE + STAGING + 2 * LARGEST];
@@ -52,7 +59,19 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
     struct Tile {
         int e, rt, ct, rows;
     };
-    auto select = [&](Tile &t) { return walk.tile(t.e, t.rt, t.ct, t.rows); };
+    // The walk's order, row tiles fastest, would pass through all rows of a large group for each of its column tiles: bands of eight row tiles instead
+    // (16384 x 1024 -> 4096: 101 -> 81 us; 8192 x 8192 x 8192 638 -> 498), so that what an XCD's workgroups share stays in its L2
+    auto select = [&](Tile &t) __attribute__((always_inline)) {
+        if (!walk.tile(t.e, t.rt, t.ct, t.rows)) return false;
+        constexpr int BAND = 8;
+        const int cnt = (t.rows + BM - 1) / BM;
+        if (cnt > BAND) {
+            const int u = t.ct * cnt + t.rt, band = u / (BAND * a.col_tiles), v = u - band * BAND * a.col_tiles, n = min(BAND, cnt - band * BAND);
+            t.ct = v / n;
+            t.rt = band * BAND + v - t.ct * n;
+        }
+        return true;
+    };
     // Per-lane indices are derived afresh wherever they are needed, from an opaque copy of the thread id, so that nothing
     // computed from them stays in registers from one part of a tile to the next.
     auto thread_id = [&]() {
@@ -64,13 +83,26 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
 
     // ---- loader.  off: this lane's byte offset from the tile's operand (xb / wb, slab 0) in each load instruction of a slab; soff, sb, sadv: the
     // same of its wave's scales
+    // (buffer loads: a scalar offset for the slab, no vector arithmetic; what lies behind the last valid row is not touched)
     uint32_t off[GPW], soff;
-    const uint8_t *xb = nullptr, *wb = nullptr, *scb = nullptr;
-    const size_t sadv = wave & 1 ? a.Ws : a.Cs;
+    struct Source {   // of a buffer resource: address and bytes, put together where it is used and through readfirstlane, since a resource in
+        uint32_t lo, hi, size;   // vector registers costs a loop around each load
+        __device__ __forceinline__ void set(const uint8_t *p, size_t bytes)
+        {
+            const uint64_t at = reinterpret_cast<uint64_t>(p);
+            lo = (uint32_t)at, hi = (uint32_t)(at >> 32), size = bytes < 0xffffffffu ? (uint32_t)bytes : 0xffffffffu;
+        }
+        __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource() const
+        {
+            const uint32_t l = __builtin_amdgcn_readfirstlane(lo), h = __builtin_amdgcn_readfirstlane(hi);
+            return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(((uint64_t)h << 32) | l), 0, (int)__builtin_amdgcn_readfirstlane(size), 0x00027000);
+        }
+    } xb = {}, wb = {}, scb = {};
+    const uint32_t sadv = wave & 1 ? a.Ws : a.Cs;
     auto set_sources = [&](const Tile &t) __attribute__((always_inline)) {
         const int row0 = t.rt * BM, col0 = t.ct * BN;
-        xb = a.x + ((size_t)t.e * a.C + row0) * pitch;
-        wb = a.w + ((size_t)t.e * a.Nout + col0) * pitch;
+        xb.set(a.x + ((size_t)t.e * a.C + row0) * pitch, (size_t)(t.rows - row0) * pitch);
+        wb.set(a.w + ((size_t)t.e * a.Nout + col0) * pitch, (size_t)(a.Nout - col0) * pitch);
         const int lane = thread_id() & 63;
         for_constants<4>([&](auto type) {
             constexpr int T = decltype(type)::value;
@@ -85,22 +117,18 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
         });
         // (selected without a branch: the compiler would move matrix instructions behind it)
         const bool w = wave & 1;
-        scb = (w ? a.ws : a.xs) + (size_t)t.e * S * sadv;
+        scb.set((w ? a.ws : a.xs) + (size_t)t.e * S * sadv, (size_t)S * sadv);
         soff = w ? t.ct * CB & ~3 : min(row0 + 4 * lane, a.Cs - 4);
     };
     // load instruction i of unit `type` of slab `slab`, into the stage `stage` bytes into LDS
     auto load_one = [&](auto type, int i, int slab, int stage) __attribute__((always_inline)) {
         constexpr int T = decltype(type)::value;
         if (T == A0 && i == kCode[A0]) {
-            uint32_t o = soff;
-            asm volatile("" : "+v"(o));
-            __builtin_amdgcn_global_load_lds(SMILE_GPTR(scb + (size_t)slab * sadv + o), SMILE_LPTR(lds + stage + SCALES + wave * 256), 4, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(scb.resource(), SMILE_LPTR(lds + stage + SCALES + wave * 256), 4, soff, slab * sadv, 0, 0);
             return;
         }
-        const uint8_t *base = (T == A0 || T == A1 ? xb : wb) + (size_t)slab * kFp8Block;
-        uint32_t o = off[kFirst[T] + min_int(i, kCode[T] - 1)];
-        asm volatile("" : "+v"(o));   // scalar base + 32-bit offset, not a 64-bit sum kept per lane
-        __builtin_amdgcn_global_load_lds(SMILE_GPTR(base + o), SMILE_LPTR(lds + stage + kOff[T] + (wave + i * NW) * 1024), 16, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds((T == A0 || T == A1 ? xb : wb).resource(), SMILE_LPTR(lds + stage + kOff[T] + (wave + i * NW) * 1024), 16,
+                                                 off[kFirst[T] + min_int(i, kCode[T] - 1)], slab * kFp8Block, 0, 0);
     };
     auto load_unit = [&](auto type, int slab, int stage) __attribute__((always_inline)) {
         for_constants<kCnt[decltype(type)::value]>([&](auto i) { load_one(type, decltype(i)::value, slab, stage); });
@@ -112,36 +140,38 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
             if (V < units) load_unit(std::integral_constant<int, V & 3>{}, V / 4, V < 4 ? stage : STAGE - stage);
         });
     };
-    // bias of this lane's columns, as it lies in memory (16-bit storage: in the first two words); without one zeros, so that the registers of the
-    // last tile's are not kept through a contraction
-    u32x4 bias_regs[TN][4];
-    auto load_bias = [&](const Tile &t) __attribute__((always_inline)) {
-        const int fhi = (thread_id() >> 5) & 1;
-        const auto at = [&](int i, int q) {
-            const int col = t.ct * BN + (i < QB ? wn * QB * 32 + i * 32 : kExt[B0] + wn * QB * 32 + (i - QB) * 32) + 8 * q + 4 * fhi;
-            return (size_t)t.e * a.Nout + min(col, a.Nout - 4);
-        };
-        if (!a.bias) {
-#pragma unroll
-            for (int k = 0; k < 4 * TN; ++k) bias_regs[k / 4][k % 4] = u32x4{0u, 0u, 0u, 0u};
-        } else if (a.dtype == SMILE_DTYPE_F32) {
-#pragma unroll
-            for (int k = 0; k < 4 * TN; ++k) bias_regs[k / 4][k % 4] = *reinterpret_cast<const u32x4 *>(static_cast<const float *>(a.bias) + at(k / 4, k % 4));
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4 * TN; ++k) {
-                const u32x2 v = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(a.bias) + at(k / 4, k % 4));
-                bias_regs[k / 4][k % 4] = u32x4{v[0], v[1], 0u, 0u};
-            }
-        }
-    };
-
     Tile cur;
     if (!select(cur)) return;
     set_sources(cur);
     int stage0 = 0;   // where the tile's slab 0 lies in LDS (0 or STAGE)
     load_first(4 * S, stage0);
-    load_bias(cur);
+
+    // The kept rows whose derivative multiplies the tile: requested in front of the next tile's units, since loads return in order.  Pieces of
+    // 16 codes per lane as the epilogue stages them, and the scales of this lane's rows.
+    constexpr int P8 = QB * 2, SLOPES = KIND == kFp8Slope ? TM * 2 : 1, SLOPE_SCALES = KIND == kFp8Slope ? TM * CB : 1;
+    constexpr int SLOPE_LOADS = KIND == kFp8Slope ? TM * 2 * (P8 / 2) + TM * CB : 0;
+    u32x4 slope[SLOPES][P8 / 2];
+    uint8_t slope_scale[SLOPE_SCALES];
+    auto request_slope = [&]() __attribute__((always_inline)) {
+        if constexpr (KIND == kFp8Slope) {
+            const int l = thread_id() & 63, blocks = (a.Nout + kFp8Block - 1) / kFp8Block;
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                const int row0 = cur.rt * BM + (j < QA0 ? j * 64 : kExt[A0] + (j - QA0) * 64) + wm * 32;
+#pragma unroll
+                for (int H = 0; H < 2; ++H)
+#pragma unroll
+                    for (int it = 0; it < P8 / 2; ++it) {   // rows and columns beyond the matrix: the last ones
+                        const int id = it * 64 + l, lrow = id / P8, row = min(row0 + lrow, cur.rows - 1);
+                        const int col = min(cur.ct * BN + H * kExt[B0] + wn * QB * 32 + (id - lrow * P8) * 16, blocks * kFp8Block - 16);
+                        slope[j * 2 + H][it] = *reinterpret_cast<const u32x4 *>(a.g8 + ((size_t)cur.e * a.C + row) * ((size_t)blocks * kFp8Block) + col);
+                    }
+#pragma unroll
+                for (int b = 0; b < CB; ++b)
+                    slope_scale[j * CB + b] = a.gs[((size_t)cur.e * blocks + min(cur.ct * CB + b, blocks - 1)) * a.Cs + min(row0 + (l & 31), cur.rows - 1)];
+            }
+        }
+    };
 
     for (;;) {
     walk.advance();
@@ -178,17 +208,12 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
     };
 
     f32x16 acc[TN][TM];
-    const auto set_acc = [&](auto value) __attribute__((always_inline)) {   // value(word of bias_regs, element 0 .. 3)
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
+    for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int j = 0; j < TM; ++j)
+        for (int j = 0; j < TM; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = value(bias_regs[i][v / 4], v % 4);
-    };
-    if (a.dtype == SMILE_DTYPE_F32) set_acc([](u32x4 w, int k) { return __uint_as_float(w[k]); });
-    else if (a.dtype == SMILE_DTYPE_BF16) set_acc([](u32x4 w, int k) { return k % 2 ? Half<__bf16>::hi(w[k / 2]) : Half<__bf16>::lo(w[k / 2]); });
-    else set_acc([](u32x4 w, int k) { return k % 2 ? Half<_Float16>::hi(w[k / 2]) : Half<_Float16>::lo(w[k / 2]); });
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
     // The products of a slab go A0 B0, A0 B1, A1 B0, A1 B1: each unit's registers are free when its next one is due.
     // Phase f: waits for unit f (every wave is then also done reading unit f - 1, whose slot is free), reads it, requests the
@@ -206,11 +231,14 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
         __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave's reads of unit f - 1
         if constexpr (D <= -7) wait_vmcnt<behind(RT, 6)>();
         else if constexpr (D < 0) {
-            wait_vmcnt<behind(RT, -1 - D) + (FOLLOWS ? behind(3, D + 7) : 0)>();
+            wait_vmcnt<behind(RT, -1 - D) + (FOLLOWS ? SLOPE_LOADS + behind(3, D + 7) : 0)>();
         }
         if constexpr (D < 1) __builtin_amdgcn_s_barrier();
         if constexpr (FOLLOWS && D >= -7 && D < 0) {
-            if constexpr (D == -7) set_sources(nxt);
+            if constexpr (D == -7) {
+                request_slope();
+                set_sources(nxt);
+            }
             load_unit(std::integral_constant<int, LT>{}, (D + 7) / 4, to);
         }
         constexpr int QA = JA < 0 ? 0 : JA == 0 ? QA0 : QA1, NQB = JB < 0 ? 0 : QB;
@@ -239,6 +267,17 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
             }
         };
         body(lds + from);
+        // The products of the last slabs have no use before the end of the tile: without this the compiler moves all of them there
+        if constexpr (JA >= 0 && D != -32) {
+#pragma unroll
+            for (int i = 0; i < QB; ++i)
+#pragma unroll
+                for (int j = 0; j < QA; ++j) {
+                    f32x16 &c = acc[JB * QB + i][(JA == 0 ? 0 : QA0) + j];
+                    if constexpr (OCC == 1) asm volatile("" : "+a"(c));
+                    else asm volatile("" : "+v"(c));
+                }
+        }
     };
     auto take_scales = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -287,12 +326,10 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
         asm volatile("; one or two slabs" ::);   // no common code with the longer ones: their last products stay in front of the joint
     }
 #undef SMILE_IC
-    if (more) {
-        if (S < 3) {   // its first units all at once; their slots were last read two phases and a barrier ago
-            set_sources(nxt);
-            load_first(4 * S, stage0);
-        }
-        load_bias(nxt);
+    if (S < 3) request_slope();
+    if (S < 3 && more) {   // its first units all at once; their slots were last read two phases and a barrier ago
+        set_sources(nxt);
+        load_first(4 * S, stage0);
     }
 
     // ---- epilogue.  Accumulator element v of a lane is (column 8*(v/4) + 4*(lane/32) + v%4, row lane%32) of its 32 x 32 block.
@@ -380,11 +417,38 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
             });
         }
     };
-    if constexpr (!ROWS8) {
+    // Bias by scalar loads, which nothing else of the tile waits for: eight columns' words, of which a lane takes its half
+    if (KIND != kFp8Slope && a.bias) {
+        const auto add_bias = [&](auto words, auto value) __attribute__((always_inline)) {   // words: of eight columns; value(words of four, k)
+            constexpr int W = decltype(words)::value;
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = min(col_at(i / QB) + i % QB * 32 + 8 * q, Nout - 8);
+                    const auto *p = (const __attribute__((address_space(4))) uint32_t *)a.bias + ((size_t)e * Nout + col) / 8 * W;
+                    uint32_t w[W / 2];
+#pragma unroll
+                    for (int k = 0; k < W / 2; ++k) {   // (through readfirstlane: a choice of addresses would be a vector load)
+                        const uint32_t even = __builtin_amdgcn_readfirstlane(p[k]), odd = __builtin_amdgcn_readfirstlane(p[W / 2 + k]);
+                        w[k] = ohi ? odd : even;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float b = value(w, k);
+#pragma unroll
+                        for (int j = 0; j < TM; ++j) acc[i][j][4 * q + k] += b;
+                    }
+                }
+        };
+        if (a.dtype == SMILE_DTYPE_F32) add_bias(std::integral_constant<int, 8>{}, [](const uint32_t *w, int k) { return __uint_as_float(w[k]); });
+        else if (a.dtype == SMILE_DTYPE_BF16) add_bias(std::integral_constant<int, 4>{}, [](const uint32_t *w, int k) { return k % 2 ? Half<__bf16>::hi(w[k / 2]) : Half<__bf16>::lo(w[k / 2]); });
+        else add_bias(std::integral_constant<int, 4>{}, [](const uint32_t *w, int k) { return k % 2 ? Half<_Float16>::hi(w[k / 2]) : Half<_Float16>::lo(w[k / 2]); });
+    }
+    if constexpr (KIND == kFp8Y) {
         activate_all();
         store_y();
     } else {
-        constexpr int P8 = QB * 2;             // 16-byte pieces of a staged row of codes
         constexpr int SROW8 = QB * 32 + 16;
         const int NB = (Nout + kFp8Block - 1) / kFp8Block, ypitch = NB * kFp8Block;
         if (cur.ct * BN + BN > Nout) {         // columns beyond the matrix are zero codes
@@ -401,19 +465,17 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
         auto store_rows8 = [&](uint8_t *codes, uint8_t *scales, lds_char *largest) __attribute__((always_inline)) {
             uint32_t mine[TM][CB];
 #pragma unroll
-            for (int j = 0; j < TM; ++j) {
-#pragma unroll
-                for (int b = 0; b < CB; ++b) mine[j][b] = 0;
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) mine[j][CB == 2 ? i / QB : 0] = max(mine[j][CB == 2 ? i / QB : 0], magnitude(acc[i][j][v]));
+            for (int j = 0; j < TM; ++j)
 #pragma unroll
                 for (int b = 0; b < CB; ++b) {
-                    mine[j][b] = max(mine[j][b], (uint32_t)__shfl_xor((int)mine[j][b], 32, 64));
-                    if (ohi == 0) *(lds_u32 *)(largest + ((wn * CB + b) * BM + row_at(j) + orow) * 4) = mine[j][b];
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int i = CB == 2 ? b * QB : 0; i < (CB == 2 ? b * QB + QB : TN); ++i)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) m = max(m, magnitude_key(acc[i][j][v]));
+                    mine[j][b] = m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+                    if (ohi == 0) *(lds_u32 *)(largest + ((wn * CB + b) * BM + row_at(j) + orow) * 4) = m;
                 }
-            }
             __builtin_amdgcn_s_waitcnt(0xC07F);
             __builtin_amdgcn_s_barrier();
             for_constants<TM>([&](auto jj) {
@@ -423,12 +485,12 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
                 uint32_t byte[CB];
 #pragma unroll
                 for (int b = 0; b < CB; ++b)
-                    byte[b] = scale_byte(max(mine[j][b], *(const lds_u32 *)(largest + (((1 - wn) * CB + b) * BM + row_at(j) + orow) * 4)));
+                    byte[b] = scale_byte(magnitude_of(max(mine[j][b], *(const lds_u32 *)(largest + (((1 - wn) * CB + b) * BM + row_at(j) + orow) * 4))));
                 for_constants<2>([&](auto part) {
                     constexpr int H = decltype(part)::value, b = CB == 2 ? H : 0;
                     const int col0 = col_at(H), block = cur.ct * CB + b;
                     if (block >= NB) return;
-                    const float r = scale_reciprocal(byte[b]);
+                    const float r = scale_value(byte[b]);
 #pragma unroll
                     for (int i = 0; i < QB; ++i)
 #pragma unroll
@@ -448,23 +510,21 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
             });
         };
         lds_char *const largest = lds + 2 * STAGE + STAGING;
-        if (a.p8) store_rows8(a.p8, a.ps, largest);
-        // times the activation's derivative at the kept pre-activation, which comes in as 8-bit rows do
+        if (KIND == kFp8Rows && a.p8) store_rows8(a.p8, a.ps, largest);
+        // times the activation's derivative at the kept rows, which take the way through LDS that 8-bit rows take out
         const auto times_slope = [&](auto post) __attribute__((always_inline)) {
             for_constants<TM>([&](auto jj) {
                 constexpr int j = decltype(jj)::value;
-                const int row0 = cur.rt * BM + row_at(j);
-                if (row0 >= rows) return;
+                if (cur.rt * BM + row_at(j) >= rows) return;
                 for_constants<2>([&](auto part) {
                     constexpr int H = decltype(part)::value, b = CB == 2 ? H : 0;
-                    const int col0 = col_at(H), block = cur.ct * CB + b;
-                    if (block >= NB) return;
+                    if (cur.ct * CB + b >= NB) return;
 #pragma unroll
                     for (int it = 0; it < P8 / 2; ++it) {
-                        const int id = it * 64 + olane, lrow = id / P8, row = min(row0 + lrow, rows - 1), at = (id - lrow * P8) * 16;
-                        *(lds_u32x4 *)(stg + lrow * SROW8 + at) = *reinterpret_cast<const u32x4 *>(a.g8 + ((size_t)e * a.C + row) * ypitch + col0 + at);
+                        const int id = it * 64 + olane, lrow = id / P8;
+                        *(lds_u32x4 *)(stg + lrow * SROW8 + (id - lrow * P8) * 16) = slope[j * 2 + H][it];
                     }
-                    const float s = scale_value(a.gs[((size_t)e * NB + block) * a.Cs + min(row0 + orow, rows - 1)]);
+                    const float s = scale_value(slope_scale[j * CB + b]);
 #pragma unroll
                     for (int i = 0; i < QB; ++i)
 #pragma unroll
@@ -477,10 +537,9 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
                 });
             });
         };
-        if (a.g8 && a.act == 1) {
-            times_slope(std::integral_constant<int, 1>{});
-        } else if (a.g8) {
-            times_slope(std::integral_constant<int, 2>{});
+        if constexpr (KIND == kFp8Slope) {
+            if (a.act == 1) times_slope(std::integral_constant<int, 1>{});
+            else times_slope(std::integral_constant<int, 2>{});
         } else {
             activate_all();
         }
@@ -491,17 +550,18 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
     cur = nxt;
     }   // tile loop
     wait_vmcnt<0>();   // what was requested once more must not land in the LDS of another workgroup
+#endif
 }
 
-template <int QA0, int QA1, int QB0, int QB1, int OCC, bool ROWS8>
+template <int QB, int OCC, int KIND>
 hipError_t launch_fp8_ring(Fp8Gemm a, const Tuning &tune, hipStream_t s)
 {
-    constexpr int BM = 64 * (QA0 + QA1), BN = 64 * (QB0 + QB1);
+    constexpr int BM = 128, BN = 128 * QB;
     a.col_tiles = (a.Nout + BN - 1) / BN;
     const long long tiles = (long long)a.N * ((a.C + BM - 1) / BM) * a.col_tiles;
     const int slots = workgroup_slots(tune, OCC);
     const int grid = tiles < slots ? (int)((tiles + 7) / 8 * 8) : slots;
-    SMILE_LAUNCH((fp8_gemm_ring_kernel<QA0, QA1, QB0, QB1, OCC, ROWS8>), dim3(grid), dim3(256), 0, s, a);
+    SMILE_LAUNCH((fp8_gemm_ring_kernel<1, 1, QB, QB, OCC, KIND>), dim3(grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

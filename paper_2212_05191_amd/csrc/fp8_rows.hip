@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void fp8_pack_weights_kernel(const void *
         float v[8];
         P::widen(raw[i], v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) largest = max(largest, magnitude(v[k]));
+        for (int k = 0; k < 8; ++k) largest = max(largest, magnitude_key(v[k]));
     }
     largest = max_of_16(largest);
     largest = max(largest, (uint32_t)__shfl_xor((int)largest, 16, 64));
@@ -109,8 +109,8 @@ __global__ __launch_bounds__(kThreads) void fp8_pack_weights_kernel(const void *
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) largest = max(largest, largest_of[i]);
-    const uint32_t byte = scale_byte(largest);
-    const float r = scale_reciprocal(byte);
+    const uint32_t byte = scale_byte(magnitude_of(largest));
+    const float r = scale_value(byte);
     const int lines = (NB + 15) / 16 * 16, lines_t = (KB + 15) / 16 * 16;
     if (threadIdx.x == 0) {
         scales[((size_t)e * KB + kb) * lines + nb] = (uint8_t)byte;
