@@ -171,10 +171,18 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _raw_stream
+        if _raw_stream is None:
+            import torch
+            # the handle itself: building a torch Stream object for it costs more than a small launch
+            raw, device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+            _raw_stream = lambda: raw(device())      # noqa: E731
+        return _raw_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -385,10 +393,15 @@ def make_backward_io(x, w_inter, w_intra, w1, w2, fwd: "LayerBuffers", dy, bwd: 
 
 # ------------------------------------------------------------------ operators in 8 bits
 
+_CODES = {}
+
+
 def _dtype_code(t) -> int:
     """DTYPE code of a torch tensor's element type."""
-    import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    if not _CODES:
+        import torch
+        _CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    code = _CODES.get(t.dtype)
     if code is None:
         raise TypeError(f"storage type {t.dtype} is none of float32, bfloat16, float16")
     return code
@@ -403,36 +416,46 @@ def smile_fp8_scale_pitch(rows: int) -> int:
 
 
 def _has_shape(name, t, shape):
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
 
 
+def _check_codes(name, codes, scales, N, rows, K, scaled):
+    """Codes [N][rows][K up to a multiple of 128] and scales [N][blocks of K][`scaled` up to a multiple of 16]: the shapes that
+    the library takes for granted."""
+    blocks = -(-K // 128)
+    _has_shape(name, codes, (N, rows, blocks * 128))
+    _has_shape(name + " scales", scales, (N, blocks, -(-scaled // 16) * 16))
+    for t in (codes, scales):
+        if t.element_size() != 1:
+            raise TypeError(f"{name} is {t.dtype}, of more than a byte")
+
+
 def _check_rows8(name, codes, scales, N, rows, K):
-    """8-bit rows [N][rows][K]: the shapes that the library takes for granted."""
-    _has_shape(name, codes, (N, rows, smile_fp8_pitch(K)))
-    _has_shape(name + " scales", scales, (N, smile_fp8_pitch(K) // 128, smile_fp8_scale_pitch(rows)))
+    _check_codes(name, codes, scales, N, rows, K, rows)
 
 
 def _check_weights8(name, codes, scales, N, Nout, K):
-    _has_shape(name, codes, (N, Nout, smile_fp8_pitch(K)))
-    _has_shape(name + " scales", scales, (N, smile_fp8_pitch(K) // 128, smile_fp8_scale_pitch(-(-Nout // 128))))
+    _check_codes(name, codes, scales, N, Nout, K, -(-Nout // 128))
 
 
-def _check_dtype(name, t, code):
-    if t is not None and _dtype_code(t) != code:
-        raise TypeError(f"{name} is {t.dtype}, of another storage type than the rest")
+def _check_like(name, t, shape, dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        _has_shape(name, t, shape)
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
 
 
-def _check_f32(name, t):
-    if t is not None and _dtype_code(t) != 0:
-        raise TypeError(f"{name} is {t.dtype}, not float32")
+def _f32():
+    if not _CODES:
+        import torch
+        _CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    return next(iter(_CODES))
 
 
 def _check_counts(rows, N):
-    import torch
-    if rows is not None and rows.dtype != torch.int32:
-        raise TypeError(f"rows is {rows.dtype}, not int32")
-    _has_shape("rows", rows, (N,))
+    if rows is not None:
+        import torch
+        _check_like("rows", rows, (N,), torch.int32)
 
 
 def alloc_fp8_rows(N, rows, K, device="cuda:0"):
@@ -453,13 +476,15 @@ def alloc_fp8_weights(N, Nout, K, device="cuda:0"):
 
 def smile_rms_norm(x, residual, weight, eps, sum=None, y=None, y8=None, y8_scale=None, rstd=None, stream=None):
     """x[T, d] (+ residual, or None) -> sum, y, 8-bit y, rstd: whichever are given."""
-    T, d = x.shape
+    shape, dtype = x.shape, x.dtype
+    T, d = shape
     code = _dtype_code(x)
-    for name, t, shape in (("residual", residual, (T, d)), ("weight", weight, (d,)), ("sum", sum, (T, d)), ("y", y, (T, d))):
-        _has_shape(name, t, shape)
-        _check_dtype(name, t, code)
-    _has_shape("rstd", rstd, (T,))
-    _check_f32("rstd", rstd)
+    _check_like("residual", residual, shape, dtype)
+    _check_like("weight", weight, (d,), dtype)
+    _check_like("sum", sum, shape, dtype)
+    _check_like("y", y, shape, dtype)
+    if rstd is not None:
+        _check_like("rstd", rstd, (T,), _f32())
     if y8 is not None:
         _check_rows8("y8", y8, y8_scale, 1, T, d)
     _check(load().smile_rms_norm(T, d, code, _ptr(x), _ptr(residual), _ptr(weight), float(eps), _ptr(sum), _ptr(y), _ptr(y8),
@@ -473,14 +498,15 @@ def smile_rms_norm_backward_workspace_bytes(T, d) -> int:
 
 
 def smile_rms_norm_backward(dy, s, weight, rstd, ds, dweight, workspace, dsum=None, stream=None):
-    T, d = dy.shape
+    shape, dtype = dy.shape, dy.dtype
+    T, d = shape
     code = _dtype_code(dy)
-    for name, t, shape in (("s", s, (T, d)), ("weight", weight, (d,)), ("ds", ds, (T, d)), ("dsum", dsum, (T, d))):
-        _has_shape(name, t, shape)
-        _check_dtype(name, t, code)
-    for name, t, shape in (("rstd", rstd, (T,)), ("dweight", dweight, (d,))):
-        _has_shape(name, t, shape)
-        _check_f32(name, t)
+    _check_like("s", s, shape, dtype)
+    _check_like("weight", weight, (d,), dtype)
+    _check_like("ds", ds, shape, dtype)
+    _check_like("dsum", dsum, shape, dtype)
+    _check_like("rstd", rstd, (T,), _f32())
+    _check_like("dweight", dweight, (d,), _f32())
     _check(load().smile_rms_norm_backward(T, d, code, _ptr(dy), _ptr(dsum), _ptr(s), _ptr(weight), _ptr(rstd), _ptr(ds),
                                           _ptr(dweight), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                           _stream(stream)), "smile_rms_norm_backward")
@@ -488,7 +514,8 @@ def smile_rms_norm_backward(dy, s, weight, rstd, ds, dweight, workspace, dsum=No
 
 def _grouped(t):
     """(N, C, K) of a tensor [N, C, K] or [C, K]"""
-    return tuple(t.shape) if t.dim() == 3 else (1, *t.shape)
+    shape = t.shape
+    return shape if len(shape) == 3 else (1, *shape)
 
 
 def smile_fp8_pack_rows(src, codes, scales, rows=None, stream=None):
@@ -543,7 +570,8 @@ def make_fp8_gemm_args(x8, x_scale, w8, w_scale, K, Nout, rows=None, act="none",
         raise ValueError(f"bias has shape {tuple(bias.shape)}, not {(N, Nout)}")
     _check_counts(rows, N)
     code = _dtype_code(y) if y is not None else _dtype_code(bias) if bias is not None else DTYPE[dtype or "bf16"]
-    _check_dtype("bias", bias, code)
+    if bias is not None and _dtype_code(bias) != code:
+        raise TypeError(f"bias is {bias.dtype}, of another storage type than y")
     args = Fp8GemmArgs(N, cap, int(K), int(Nout), code, ACT[act])
     tensors = dict(x8=x8, x_scale=x_scale, w8=w8, w_scale=w_scale, bias=bias, rows=rows, y=y, y8=y8, y_scale=y_scale, pre8=pre8,
                    pre_scale=pre_scale, grad8=grad8, grad_scale=grad_scale)
@@ -572,7 +600,8 @@ def smile_fp8_weight_grad(dy, x8, x_scale, dw, workspace, rows=None, stream=None
     if _grouped(dw) != (N, Nout, K):
         raise ValueError(f"dw has shape {tuple(dw.shape)}, not {(N, Nout, K)}")
     _check_rows8("x8", x8, x_scale, N, cap, K)
-    _check_dtype("dw", dw, _dtype_code(dy))
+    if dw.dtype != dy.dtype:
+        raise TypeError(f"dw is {dw.dtype}, dy {dy.dtype}")
     _check_counts(rows, N)
     _check(load().smile_fp8_weight_grad(N, cap, Nout, K, _dtype_code(dy), _ptr(dy), _ptr(x8), _ptr(x_scale), _ptr(rows), _ptr(dw),
                                         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),

@@ -1,4 +1,5 @@
 // C-ABI entry points of the 8-bit operators: argument checks, all of them on the host before anything is enqueued.
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <cmath>
@@ -201,11 +202,14 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
     // (exactly, in bfloat16) and multiplied by the gradient kernels of the expert FFN.
     hipError_t err = launch_fp8_unpack_rows(dtype, RowsIo{N, C, K, rows}, static_cast<const uint8_t *>(x8), static_cast<const uint8_t *>(x_scale), workspace, s);
     if (err != hipSuccess) return from_hip(err);
+    // Row counts that the device knows: buffers are made a quarter larger than what they expect (capacity factor 1.25).  The rules of the gradient
+    // kernels go by it: 64 groups of 256 rows in buffers of 320, 1024 x 4096: 280 -> 266 us.
+    const int tokens = rows ? (int)std::max(1ll, (long long)N * C * 4 / 5) : 0;
     const long long sx = (long long)C * Nout, sw = (long long)C * K, sy = (long long)Nout * K;
     if (is_half(dtype)) {
         TransposedGemm g{};
         g.x = dy, g.w = workspace, g.y = dw, g.k_valid = rows, g.N = N, g.Mrows = Nout, g.Nout = K, g.K = C, g.ldx = Nout, g.ldw = K;
-        g.sx = sx, g.sw = sw, g.sy = sy, g.x_transposed = g.w_transposed = true, g.tune = device_tuning();
+        g.sx = sx, g.sw = sw, g.sy = sy, g.x_transposed = g.w_transposed = true, g.tune = device_tuning(), g.tokens = tokens;
         return from_hip(launch_grouped_gemm_t(dtype, g, s));
     }
     F32Gemm g{};

@@ -193,24 +193,45 @@ __global__ __launch_bounds__(kThreads) void rms_norm_backward_kernel(RmsNormGrad
     }
 }
 
-// dweight[c] = sum of the workgroups' parts, 16 columns a workgroup: thread (c, q) adds parts q, q + 16, ... in order, then the sixteen are
-// added in order, in 64 bits (a column has up to some thousand parts of either sign).
-__global__ __launch_bounds__(kThreads) void rms_norm_dweight_kernel(const float *__restrict__ part, float *__restrict__ dweight, int parts, int d)
+// dweight[c] = sum of the workgroups' parts, 16 columns a workgroup: thread (c, q) adds parts q, q + 64, ... in order, eight loads in flight, then the
+// 64 are added in order, in 64 bits (a column has up to some thousand parts of either sign).
+__global__ __launch_bounds__(1024) void rms_norm_dweight_kernel(const float *__restrict__ part, float *__restrict__ dweight, int parts, int d)
 {
-    __shared__ double lds[16][16];
-    const int c = blockIdx.x * 16 + threadIdx.x % 16, q = threadIdx.x / 16;
+    __shared__ double lds[64][17];
+    const int lc = threadIdx.x % 16, c = blockIdx.x * 16 + lc, q = threadIdx.x / 16;
     double v = 0.;
-    if (c < d)
-        for (int p = q; p < parts; p += 16) v += (double)part[(size_t)p * d + c];
-    lds[q][threadIdx.x % 16] = v;
+    if (c < d) {
+        int p = q;
+        for (; p + 7 * 64 < parts; p += 8 * 64) {
+            float a[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = part[(size_t)(p + i * 64) * d + c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += (double)a[i];
+        }
+        for (; p < parts; p += 64) v += (double)part[(size_t)p * d + c];
+    }
+    lds[q][lc] = v;
+    __syncthreads();
+    if (q < 8) {
+        v = 0.;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += lds[q * 8 + k][lc];
+    }
+    __syncthreads();
+    if (q < 8) lds[q][lc] = v;
     __syncthreads();
     if (q == 0 && c < d) {
-        for (int k = 1; k < 16; ++k) v += lds[k][threadIdx.x % 16];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) v += lds[k][lc];
         dweight[c] = (float)v;
     }
 }
 
-constexpr int kGradBlocks = 1024;   // workgroups of the backward kernel at most: parts of dw
+// Workgroups at most, each of consecutive rows: four a CU forward, three backward, whose registers leave no room for a fourth and whose number is that
+// of the parts of dw.  us, 65536 x 1024 bf16, y alone: 768 116, 1024 103, 1280 111, 2048 108 (a copy of its bytes: 104); y8 alone 105, 92, 100, 98
+// (91); backward 512 114, 768 113, 1024 113, 4096 118 (104); 16384 x 1024: 28.3, 25.9, 27.3, 36.4 (26.0); 5003 x 960 fp16 12.4, 11.9, 11.9, 15.2 (7.4).
+constexpr int kForwardBlocks = 1024, kGradBlocks = 768;
 
 struct NormShape {
     int lanes, pieces;
@@ -232,15 +253,14 @@ hipError_t launch_shape(const RmsNormIo *f, const RmsNormGradIo *g, hipStream_t 
 {
     constexpr int GROUPS = kThreads / LPR;
     const int T = f ? f->T : g->T;
-    // four workgroups a CU, at most, of consecutive rows
-    const int blocks = min_int((T + GROUPS - 1) / GROUPS, kGradBlocks);
+    const int blocks = min_int((T + GROUPS - 1) / GROUPS, f ? kForwardBlocks : kGradBlocks);
     const int per = (T + blocks * GROUPS - 1) / (blocks * GROUPS);
     const int grid = (T + GROUPS * per - 1) / (GROUPS * per);
     if (f) {
         SMILE_LAUNCH((rms_norm_kernel<DT, LPR, NP>), dim3(grid), dim3(kThreads), 0, s, *f, per);
     } else {
         SMILE_LAUNCH((rms_norm_backward_kernel<DT, LPR, NP>), dim3(grid), dim3(kThreads), 0, s, *g, per);
-        SMILE_LAUNCH(rms_norm_dweight_kernel, dim3((g->d + 15) / 16), dim3(kThreads), 0, s, (const float *)g->partial, g->dweight, grid, g->d);
+        SMILE_LAUNCH(rms_norm_dweight_kernel, dim3((g->d + 15) / 16), dim3(1024), 0, s, (const float *)g->partial, g->dweight, grid, g->d);
     }
     return hipGetLastError();
 }
