@@ -13,7 +13,7 @@ namespace smile {
 namespace {
 
 constexpr int kWidest = 32768, kWidestNorm = 16384;
-constexpr long long kMostRows = 1ll << 30;
+constexpr long long kMostRows = 1ll << 27;          // (32 lanes a row, 2^32 threads a launch)
 constexpr double kMostElements = 1099511627776.0;   // 2^40
 
 bool known(int dtype) { return dtype == SMILE_DTYPE_F32 || dtype == SMILE_DTYPE_BF16 || dtype == SMILE_DTYPE_F16; }
@@ -24,6 +24,7 @@ smile_status check_rows(int N, int C, int width, int dtype)
     if (!known(dtype)) return SMILE_UNSUPPORTED;
     if (N < 1 || C < 1 || width < 8 || width % 8 || width > kWidest || N > 4096) return SMILE_BAD_SHAPE;
     if ((long long)N * C > kMostRows || (double)N * C * fp8_pitch(width) >= kMostElements) return SMILE_BAD_SHAPE;
+    if ((long long)fp8_blocks(width) * fp8_scale_pitch(C) >= 1ll << 31) return SMILE_BAD_SHAPE;   // the scales of a group, in 32 bits
     return SMILE_OK;
 }
 

@@ -24,6 +24,14 @@ namespace {
 __device__ __forceinline__ uint32_t magnitude_key(float v) { return (__float_as_uint(v) << 1) + 0x01000000u; }
 __device__ __forceinline__ uint32_t magnitude_of(uint32_t key) { return (max(key, 0x01000000u) - 0x01000000u) >> 1; }
 
+// max(m, |a|, |b|), NaN passed over, infinities not (half an instruction a value)
+__device__ __forceinline__ float max_magnitude(float m, float a, float b)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(m), "v"(a), "v"(b));
+    return r;
+}
+
 // The scale's byte for a block's largest magnitude m 2^p (as bits): 2^(p-8) if m <= 1.75 (448 = 1.75 * 2^8), else 2^(p-7).  At least 1, the
 // smallest normal power; at most 247.
 __device__ __forceinline__ uint32_t scale_byte(uint32_t largest)

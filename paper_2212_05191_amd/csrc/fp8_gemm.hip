@@ -6,8 +6,6 @@
 // instructions, four blocks of 128 ahead: a lane holds row (or column) lane % 32 and the half lane / 32 of its 128 bytes.  The order of
 // the k inside a block does not matter as long as both operands have the same.  The waves' sums meet in LDS in a fixed order, and the
 // epilogue works on runs of eight columns, sixteen lanes to a block of the 8-bit outputs.
-#include <algorithm>
-
 #include "fp8_gemm_ring.hpp"
 
 namespace smile {
@@ -159,10 +157,17 @@ hipError_t launch_rows(Fp8Gemm a, hipStream_t s)
 {
     a.row_tiles = (a.C + 31) / 32;
     a.col_tiles = (a.Nout + 32 * WN - 1) / (32 * WN);
-    const long long tiles = (long long)a.N * a.row_tiles * a.col_tiles;
-    if (tiles >= 1ll << 31) return hipErrorInvalidValue;
+    const long long tiles = (long long)a.N * a.row_tiles * a.col_tiles;   // (few, by the rule below)
     SMILE_LAUNCH((fp8_gemm_rows_kernel<WN, WK, ROWS8>), dim3((unsigned)tiles), dim3(64 * WN * WK), 0, s, a);
     return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t launch_act(const Fp8Gemm &g, const Tuning &tune, hipStream_t s)
+{
+    if (g.act == 1) return launch_fp8_ring<1, 2, KIND, 1>(g, tune, s);
+    if (g.act == 3) return launch_fp8_ring<1, 2, KIND, 3>(g, tune, s);
+    return launch_fp8_ring<1, 2, KIND, 0>(g, tune, s);
 }
 
 }  // namespace
@@ -182,13 +187,12 @@ hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s)
     const auto tiles = [&](int rows, int columns) {
         return (long long)g.N * ((g.C + rows - 1) / rows) * ((g.Nout + columns - 1) / columns);
     };
-    // (the ring kernels' scale offsets are 32 bits)
-    if ((long long)g.KB * std::max(g.Cs, g.Ws) >= 1ll << 31 || (rows8 ? g.KB <= 4 && tiles(32, 128) <= tune.cus : tiles(32, 32) <= 2 * tune.cus))
+    if (rows8 ? g.KB <= 4 && tiles(32, 128) <= tune.cus : tiles(32, 32) <= 2 * tune.cus)
         return rows8 ? launch_rows<4, 2, true>(g, s) : launch_rows<1, 4, false>(g, s);
-    if (g.g8) return launch_fp8_ring<1, 2, kFp8Slope>(g, tune, s);
-    if (rows8) return launch_fp8_ring<1, 2, kFp8Rows>(g, tune, s);
-    if (g.act == 0 && g.KB >= 16 && tiles(128, 256) >= 4 * tune.cus) return launch_fp8_ring<2, 1, kFp8Y>(g, tune, s);
-    return launch_fp8_ring<1, 2, kFp8Y>(g, tune, s);
+    if (g.g8) return g.act == 1 ? launch_fp8_ring<1, 2, kFp8Slope, 1>(g, tune, s) : launch_fp8_ring<1, 2, kFp8Slope, 3>(g, tune, s);
+    if (rows8) return launch_act<kFp8Rows>(g, tune, s);
+    if (g.act == 0 && g.KB >= 16 && tiles(128, 256) >= 4 * tune.cus) return launch_fp8_ring<2, 1, kFp8Y, 0>(g, tune, s);
+    return launch_act<kFp8Y>(g, tune, s);
 }
 
 }  // namespace smile

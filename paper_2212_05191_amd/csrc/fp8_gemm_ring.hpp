@@ -27,8 +27,9 @@ namespace {
 
 enum { kFp8Y, kFp8Rows, kFp8Slope };   // y alone; 8-bit rows too; both times the activation's derivative at kept 8-bit rows
 
-// QA0, QA1 / QB0, QB1: 32-wide blocks per wave in the units A0, A1 / B0, B1.  KIND: what the epilogue does.
-template <int QA0, int QA1, int QB0, int QB1, int OCC, int KIND>
+// QA0, QA1 / QB0, QB1: 32-wide blocks per wave in the units A0, A1 / B0, B1.  KIND: what the epilogue does.  ACT: the activation, 0 none, 1 ReLU, 3 GELU
+// (of the kernel, not of the call: the branches would copy every accumulator).
+template <int QA0, int QA1, int QB0, int QB1, int OCC, int KIND, int ACT>
 __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host has no type for a buffer resource)
@@ -339,23 +340,12 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
     auto row_at = [&](int j) { return (j < QA0 ? j * 64 : kExt[A0] + (j - QA0) * 64) + wm * 32; };            // first row of block j in the tile
     auto col_at = [&](int H) { return cur.ct * BN + H * kExt[B0] + wn * QB * 32; };                           // first column of part H
     auto activate_all = [&]() __attribute__((always_inline)) {
-        if (a.act == 1) {
 #pragma unroll
-            for (int i = 0; i < TN; ++i)
+        for (int i = 0; i < TN; ++i)
 #pragma unroll
-                for (int j = 0; j < TM; ++j)
+            for (int j = 0; j < TM; ++j)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[i][j][v] = activate<1>(acc[i][j][v]);
-        } else if (a.act == 3) {
-            for_constants<TM>([&](auto jj) {
-                constexpr int j = decltype(jj)::value;
-                if (cur.rt * BM + row_at(j) >= rows) return;
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[i][j][v] = activate<3>(acc[i][j][v]);
-            });
-        }
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = activate<ACT>(acc[i][j][v]);
     };
     // y: rounded, staged as [32 rows][QB * 32 columns] of 16 bits (or half as many columns of fp32), stored row-contiguously
     auto store_y = [&]() __attribute__((always_inline)) {
@@ -463,18 +453,39 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
         }
         // The tile as 8-bit rows: each wave's largest magnitudes meet those of the wave that has the rest of the block's columns
         auto store_rows8 = [&](uint8_t *codes, uint8_t *scales, lds_char *largest) __attribute__((always_inline)) {
-            uint32_t mine[TM][CB];
+            uint32_t mine[TM][CB];   // magnitude_key's
+            bool infinite = false;
 #pragma unroll
             for (int j = 0; j < TM; ++j)
 #pragma unroll
                 for (int b = 0; b < CB; ++b) {
-                    uint32_t m = 0;
+                    float m = 0.f;
 #pragma unroll
                     for (int i = CB == 2 ? b * QB : 0; i < (CB == 2 ? b * QB + QB : TN); ++i)
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) m = max(m, magnitude_key(acc[i][j][v]));
-                    mine[j][b] = m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
-                    if (ohi == 0) *(lds_u32 *)(largest + ((wn * CB + b) * BM + row_at(j) + orow) * 4) = m;
+                        for (int v = 0; v < 16; v += 2) m = max_magnitude(m, acc[i][j][v], acc[i][j][v + 1]);
+                    mine[j][b] = magnitude_key(m);
+                    infinite |= __float_as_uint(m) >= 0x7f800000u;
+                }
+            if (__any(infinite)) {   // infinities do not count
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) {
+                        uint32_t m = 0;
+#pragma unroll
+                        for (int i = CB == 2 ? b * QB : 0; i < (CB == 2 ? b * QB + QB : TN); ++i)
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) m = max(m, magnitude_key(acc[i][j][v]));
+                        mine[j][b] = m;
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < TM; ++j)
+#pragma unroll
+                for (int b = 0; b < CB; ++b) {
+                    mine[j][b] = max(mine[j][b], (uint32_t)__shfl_xor((int)mine[j][b], 32, 64));
+                    if (ohi == 0) *(lds_u32 *)(largest + ((wn * CB + b) * BM + row_at(j) + orow) * 4) = mine[j][b];
                 }
             __builtin_amdgcn_s_waitcnt(0xC07F);
             __builtin_amdgcn_s_barrier();
@@ -538,8 +549,7 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
             });
         };
         if constexpr (KIND == kFp8Slope) {
-            if (a.act == 1) times_slope(std::integral_constant<int, 1>{});
-            else times_slope(std::integral_constant<int, 2>{});
+            times_slope(std::integral_constant<int, ACT == 1 ? 1 : 2>{});
         } else {
             activate_all();
         }
@@ -553,7 +563,7 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
 #endif
 }
 
-template <int QB, int OCC, int KIND>
+template <int QB, int OCC, int KIND, int ACT>
 hipError_t launch_fp8_ring(Fp8Gemm a, const Tuning &tune, hipStream_t s)
 {
     constexpr int BM = 128, BN = 128 * QB;
@@ -561,7 +571,7 @@ hipError_t launch_fp8_ring(Fp8Gemm a, const Tuning &tune, hipStream_t s)
     const long long tiles = (long long)a.N * ((a.C + BM - 1) / BM) * a.col_tiles;
     const int slots = workgroup_slots(tune, OCC);
     const int grid = tiles < slots ? (int)((tiles + 7) / 8 * 8) : slots;
-    SMILE_LAUNCH((fp8_gemm_ring_kernel<1, 1, QB, QB, OCC, KIND>), dim3(grid), dim3(256), 0, s, a);
+    SMILE_LAUNCH((fp8_gemm_ring_kernel<1, 1, QB, QB, OCC, KIND, ACT>), dim3(grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
