@@ -199,8 +199,15 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
     if (st != SMILE_OK) return st;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < weight_grad_workspace(N, C, K, dtype)) return SMILE_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    // The scales vary along the contraction, which is over rows, so the 8-bit matrix instructions cannot take them: the operand is widened
-    // (exactly, in bfloat16) and multiplied by the gradient kernels of the expert FFN.
+    const Tuning tune = device_tuning();
+    if (fp8_weight_grad_applies(dtype, N, C, Nout, K, tune)) {
+        Fp8WeightGrad g{};
+        g.dy = static_cast<const uint16_t *>(dy), g.x = static_cast<const uint8_t *>(x8), g.xs = static_cast<const uint8_t *>(x_scale);
+        g.rows = rows, g.dw = static_cast<uint16_t *>(dw), g.N = N, g.C = C, g.Nout = Nout, g.K = K, g.KB = fp8_blocks(K), g.Cs = fp8_scale_pitch(C);
+        return from_hip(launch_fp8_weight_grad(g, s));
+    }
+    // Half precision, which does not hold every product of a code and a scale, fp32, and few tiles: the operand is widened and multiplied by the gradient
+    // kernels of the expert FFN.
     hipError_t err = launch_fp8_unpack_rows(dtype, RowsIo{N, C, K, rows}, static_cast<const uint8_t *>(x8), static_cast<const uint8_t *>(x_scale), workspace, s);
     if (err != hipSuccess) return from_hip(err);
     // Row counts that the device knows: buffers are made a quarter larger than what they expect (capacity factor 1.25).  The rules of the gradient
@@ -210,12 +217,12 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
     if (is_half(dtype)) {
         TransposedGemm g{};
         g.x = dy, g.w = workspace, g.y = dw, g.k_valid = rows, g.N = N, g.Mrows = Nout, g.Nout = K, g.K = C, g.ldx = Nout, g.ldw = K;
-        g.sx = sx, g.sw = sw, g.sy = sy, g.x_transposed = g.w_transposed = true, g.tune = device_tuning(), g.tokens = tokens;
+        g.sx = sx, g.sw = sw, g.sy = sy, g.x_transposed = g.w_transposed = true, g.tune = tune, g.tokens = tokens;
         return from_hip(launch_grouped_gemm_t(dtype, g, s));
     }
     F32Gemm g{};
     g.x = dy, g.w = workspace, g.y = dw, g.k_valid = rows, g.N = N, g.Mrows = Nout, g.Nout = K, g.K = C, g.ldx = Nout, g.ldw = K;
-    g.sx = sx, g.sw = sw, g.sy = sy, g.x_transposed = g.w_transposed = true, g.tune = device_tuning();
+    g.sx = sx, g.sw = sw, g.sy = sy, g.x_transposed = g.w_transposed = true, g.tune = tune;
     return from_hip(launch_grouped_gemm_f32(g, s));
 }
 

@@ -54,4 +54,16 @@ struct Fp8Gemm {
 };
 hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s);
 
+// Weight gradients from 8-bit rows without a widened copy
+struct Fp8WeightGrad {
+    const uint16_t *dy;              // [N][C][Nout] bfloat16
+    const uint8_t *x, *xs;           // 8-bit rows [N][C][K]
+    const int32_t *rows;
+    uint16_t *dw;                    // [N][Nout][K]
+    int N, C, Nout, K, KB, Cs;
+    int o_tiles, k_tiles, tiles, chunk;
+};
+bool fp8_weight_grad_applies(int dtype, int N, int C, int Nout, int K, const Tuning &tune);
+hipError_t launch_fp8_weight_grad(Fp8WeightGrad a, hipStream_t s);
+
 }  // namespace smile

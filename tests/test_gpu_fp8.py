@@ -383,7 +383,9 @@ def test_gemm_of_codes_spread_over_all_exponents(C, K):
 # ------------------------------------------------------------------ weight gradient
 
 @pytest.mark.parametrize("dtype", ("bf16", "f16", "f32"))
-@pytest.mark.parametrize("N,C,Nout,K,rows", [(1, 1, 64, 64, None), (3, 17, 128, 192, (17, 0, 5)), (2, 300, 320, 960, (300, 129)), (1, 700, 64, 1600, None)])
+@pytest.mark.parametrize("N,C,Nout,K,rows", [(1, 1, 64, 64, None), (3, 17, 128, 192, (17, 0, 5)), (2, 300, 320, 960, (300, 129)), (1, 700, 64, 1600, None),
+                                             # many tiles: bfloat16 without a widened copy
+                                             (130, 70, 192, 320, tuple(k % 73 for k in range(130))), (256, 33, 64, 128, None), (33, 100, 320, 704, tuple(3 * k for k in range(33)))])
 def test_weight_grad(dtype, N, C, Nout, K, rows):
     r = np.random.default_rng(C + K)
     (x8, xs), x = packed(r.standard_normal((N, C, K)) * np.exp(r.uniform(-1, 1, (N, C, 1))))
