@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libsmile.so")
 PEAKS = os.path.join(HERE, "peaks_probe")
 SOURCES = ["smile_api.hip", "gate_logits.hip", "route.hip", "permute.hip", "expert_ffn.hip", "gemm_ring_forward.hip", "aux_loss.hip",
            "backward.hip", "gemm_transposed.hip", "gemm_ring_gradient.hip", "gemm_f32.hip", "router_grad_mfma.hip", "static_scratch.hip",
-           "rms_norm.hip", "fp8_rows.hip", "fp8_gemm.hip", "fp8_weight_grad.hip", "fp8_api.hip"]
+           "rms_norm.hip", "fp8_rows.hip", "fp8_gemm.hip", "fp8_checkpoint.hip", "fp8_weight_grad.hip", "fp8_api.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

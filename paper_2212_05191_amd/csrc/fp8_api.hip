@@ -175,7 +175,9 @@ smile_status smile_fp8_gemm(const smile_fp8_gemm_args *p, void *stream)
     g.N = a.N, g.C = a.C, g.Nout = a.Nout, g.KB = fp8_blocks(a.K);
     g.Cs = fp8_scale_pitch(a.C), g.Ws = fp8_scale_pitch(fp8_blocks(a.Nout));
     g.dtype = a.dtype, g.act = a.act == SMILE_ACT_NONE ? 0 : a.act == SMILE_ACT_RELU ? 1 : 3;
-    return from_hip(launch_fp8_gemm(g, device_tuning(), static_cast<hipStream_t>(stream)));
+    hipError_t err = launch_fp8_gemm(g, device_tuning(), static_cast<hipStream_t>(stream));
+    if (err == hipSuccess && g.p8 && g.act == 1) err = launch_fp8_near_zero(g, static_cast<hipStream_t>(stream));
+    return from_hip(err);
 }
 
 smile_status smile_fp8_weight_grad_workspace_bytes(int32_t N, int32_t C, int32_t K, int32_t dtype, size_t *bytes)

@@ -53,6 +53,7 @@ struct Fp8Gemm {
     bool backwards;                  // ring kernels: walk the tiles from the last group to the first
 };
 hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s);
+hipError_t launch_fp8_near_zero(const Fp8Gemm &g, hipStream_t s);   // after a product with p8: its codes next to zero from exact sums
 
 // Weight gradients from 8-bit rows without a widened copy
 struct Fp8WeightGrad {

@@ -380,6 +380,30 @@ def test_gemm_of_codes_spread_over_all_exponents(C, K):
     assert np.linalg.norm(host(out)[0] - want) <= 2.0 ** -12 * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("N,C,K,Nout,rows,bias", [(16, 20, 1024, 4096, None, False), (3, 400, 768, 3000, (400, 0, 257), False), (2, 350, 1032, 2056, (340, 350), True)])
+def test_checkpoint_of_relu_keeps_the_side_of_zero(N, C, K, Nout, rows, bias):
+    """ReLU's derivative is one or zero by the kept pre-activation: none may be rounded over the border by the product's own error."""
+    r = np.random.default_rng(N * C)
+    (x8, xs), x = packed(r.standard_normal((N, C, K)) * np.exp(r.uniform(-2, 2, (N, C, 1))))
+    (w8, wsc), w = packed(0.05 * r.standard_normal((N, Nout, K)), True)
+    b = stored(0.01 * r.standard_normal((N, Nout)), "bf16") if bias else None
+    counts = None if rows is None else dev(np.array(rows, np.int32))
+    out = torch.zeros((N, C, Nout), dtype=torch.bfloat16, device="cuda:0")
+    p8, ps = B.alloc_fp8_rows(N, C, Nout)
+    p8.fill_(0xAA), ps.fill_(0xAA)
+    B.smile_fp8_gemm(B.make_fp8_gemm_args(x8, xs, w8, wsc, K, Nout, rows=counts, act="relu", bias=None if b is None else dev(b, "bf16"), y=out,
+                                          pre8=p8, pre_scale=ps, dtype="bf16"))
+    for e in range(N):
+        n = C if rows is None else rows[e]
+        c, s = host(p8[e]), host(ps[e])
+        assert np.all(c[n:] == 0xAA) and np.all(s[:, n:C] == 0xAA) and np.all(c[:n, Nout:] == 0)
+        exact = x[e, :n] @ w[e].T + (0.0 if b is None else b[e])      # codes and scales: without a rounding that matters here
+        step = np.repeat(2.0 ** (s[:, :n].T.astype(np.float64) - 127), 128, axis=1)[:, :Nout]
+        got = c[:n, :Nout]
+        wrong = ((got > 0) & (got < 0x80)) != (exact > 2.0 ** -10 * step)
+        assert not wrong.any(), (e, int(wrong.sum()), np.argwhere(wrong)[:4], exact[wrong][:4])
+
+
 # ------------------------------------------------------------------ weight gradient
 
 @pytest.mark.parametrize("dtype", ("bf16", "f16", "f32"))
