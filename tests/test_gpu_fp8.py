@@ -433,6 +433,26 @@ def test_weight_grad(dtype, N, C, Nout, K, rows):
         near(got[e], want, half(want, dtype) + (n + 1) * 2.0 ** -23 * size + operand, ("dw", e))
 
 
+@pytest.mark.parametrize("N,C,Nout,K", [(256, 40, 64, 192), (300, 65, 128, 256)])
+def test_weight_grad_passes_over_scales_beyond_the_rows(N, C, Nout, K):
+    """Scales of rows that are not there may be anything, NaN's byte too; those of neighbouring rows differ by many powers of two."""
+    r = np.random.default_rng(N)
+    rows = r.integers(0, C + 1, N)
+    (x8, xs), x = packed(r.standard_normal((N, C, K)) * np.exp2(r.integers(-40, 41, (N, C, 1))))
+    dy = stored(r.standard_normal((N, C, Nout)), "bf16")
+    for e in range(N):
+        x8[e, rows[e]:] = 0x7f
+        xs[e, :, rows[e]:] = 0xff
+    dw = torch.full((N, Nout, K), 77.0, dtype=torch.bfloat16, device="cuda:0")
+    ws = torch.empty(B.smile_fp8_weight_grad_workspace_bytes(N, C, K, "bf16"), dtype=torch.uint8, device="cuda:0")
+    B.smile_fp8_weight_grad(dev(dy, "bf16"), x8, xs, dw, ws, rows=dev(rows.astype(np.int32)))
+    got = host(dw)
+    for e in range(N):
+        n = rows[e]
+        want, size = dy[e, :n].T @ x[e, :n], np.abs(dy[e, :n]).T @ np.abs(x[e, :n])
+        near(got[e], want, half(want, "bf16") + (n + 1) * 2.0 ** -23 * size, ("dw", e))
+
+
 # ------------------------------------------------------------------ streams and graphs
 
 def test_other_stream_and_graph_replays():
