@@ -324,6 +324,14 @@ def test_gemm_types_and_epilogues(dtype, C, act, bias):
         gemm_case(2, C, 520, 328, dtype, act, False, rows, y=False, y8=True, grad=True)
 
 
+@pytest.mark.parametrize("N,C,K,Nout", [(40, 9, 520, 1032), (150, 1, 136, 72), (37, 32, 1024, 640)])
+def test_gemm_many_groups_of_few_rows(N, C, K, Nout):
+    rows = tuple((5 * k) % (C + 2) for k in range(N))
+    gemm_case(N, C, K, Nout, rows=rows, act="gelu", bias=True, y=False, y8=True, pre8=True)
+    gemm_case(N, C, K, Nout, "f16", rows=rows, act="relu", bias=True, y8=True)
+    gemm_case(N, C, K, Nout, rows=rows, act="gelu", y8=True, grad=True)
+
+
 @pytest.mark.parametrize("C", (7, 200))
 def test_gemm_keeps_nan_to_its_row_and_column(C):
     r = np.random.default_rng(C)
