@@ -461,6 +461,25 @@ def test_weight_grad_passes_over_scales_beyond_the_rows(N, C, Nout, K):
         near(got[e], want, half(want, "bf16") + (n + 1) * 2.0 ** -23 * size, ("dw", e))
 
 
+@pytest.mark.parametrize("N", (1, 260))
+def test_weight_grad_in_half_precision_at_the_ends_of_its_range(N):
+    """Operands beyond 65504 count as that, products beyond it are infinite, NaN stays NaN, subnormals are kept."""
+    C, Nout, K = 5, 64, 128
+    x = np.zeros((N, C, K))
+    x[:, 0, :8], x[:, 1, :8], x[:, 2, 8:16], x[:, 3, 16:24] = 65536.0, -65536.0, 2.0 ** -20, 3.0
+    (x8, xs), _ = packed(x)
+    x8[:, 4, 30] = 0x7f
+    dy = np.zeros((N, C, Nout))
+    dy[:, 0, 0], dy[:, 1, 1], dy[:, 0, 2], dy[:, 2, 3], dy[:, 3, 4], dy[:, 4, 5] = 0.5, 1.0, 4.0, 2.0, 1.0, 1.0
+    dw = torch.zeros((N, Nout, K), dtype=torch.float16, device="cuda:0")
+    ws = torch.empty(B.smile_fp8_weight_grad_workspace_bytes(N, C, K, "f16"), dtype=torch.uint8, device="cuda:0")
+    B.smile_fp8_weight_grad(dev(dy, "f16"), x8, xs, dw, ws)
+    want = np.zeros((N, Nout, K))
+    want[:, 0, :8], want[:, 1, :8], want[:, 2, :8], want[:, 3, 8:16], want[:, 4, 16:24] = 32752.0, -65504.0, np.inf, 2.0 ** -19, 3.0
+    want[:, :, 30] = np.nan
+    assert np.array_equal(host(dw), want, equal_nan=True)
+
+
 # ------------------------------------------------------------------ streams and graphs
 
 def test_other_stream_and_graph_replays():
