@@ -531,3 +531,42 @@ def test_other_stream_and_graph_replays():
         torch.cuda.synchronize()
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(result(), eager)), k
+
+
+def test_graph_replays_of_a_relu_checkpoint_and_the_gradient_of_many_tiles():
+    r = np.random.default_rng(3)
+    N, C, K, Nout = 24, 70, 256, 512
+    (x8, xs), _ = packed(r.standard_normal((N, C, K)))
+    (w8, wsc), _ = packed(0.05 * r.standard_normal((N, Nout, K)), True)
+    dy = dev(stored(r.standard_normal((N, C, Nout)), "bf16"), "bf16")
+    rows = dev(r.integers(0, C + 1, N).astype(np.int32))
+    h8, p8 = B.alloc_fp8_rows(N, C, Nout), B.alloc_fp8_rows(N, C, Nout)
+    dw = torch.empty((N, Nout, K), dtype=torch.bfloat16, device="cuda:0")
+    ws = torch.empty(B.smile_fp8_weight_grad_workspace_bytes(N, C, K, "bf16"), dtype=torch.uint8, device="cuda:0")
+    args = B.make_fp8_gemm_args(x8, xs, w8, wsc, K, Nout, rows=rows, act="relu", y8=h8[0], y_scale=h8[1], pre8=p8[0], pre_scale=p8[1], dtype="bf16")
+    results = (*h8, *p8, dw)
+
+    def step():
+        B.smile_fp8_gemm(args)
+        B.smile_fp8_weight_grad(dy, x8, xs, dw, ws, rows=rows)
+
+    def clear():
+        for t in results:
+            t.fill_(1)
+
+    clear()
+    step()
+    want = [t.clone() for t in results]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        clear()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(results, want))
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, w) for t, w in zip(results, want))
