@@ -3,7 +3,7 @@
 // Of such a row only the side of zero is read: the derivative is one where the code is positive, else zero.  The matrix cores leave an error of some 1.5e-5
 // of a row's typical sum (fp8_gemm.hip), which moves about four elements in a million over that border, and each of them gives
 // or takes a whole term of the gradients: with few rows in a group that is a good part of a weight's gradient.  So every code whose magnitude is below
-// 2^-5 of 448 (exponent field 0 or 1: three in ten thousand of normally distributed sums, several times the error) is replaced by the code of the sum in 64 bits, where
+// 2^-5, where the largest is up to 448 (exponent field 0 or 1: three in ten thousand of normally distributed sums, several times the error) is replaced by the code of the sum in 64 bits, where
 // the products of codes and their sums are exact for all that matters.
 //
 // One wave reads 1024 codes of a row, 16 a lane, and takes the near ones in turn, all lanes along the contraction.  What bounds it are the
