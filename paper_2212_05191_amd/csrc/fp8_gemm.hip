@@ -181,18 +181,25 @@ hipError_t launch_act(const Fp8Gemm &g, const Tuning &tune, hipStream_t s)
 //   * else 128 x 128, two on a CU; 128 x 256, which moves a quarter less through L2, for long contractions without an epilogue that the other workgroup
 //     would hide, where there are four rounds of such tiles: 8192 x 8192 x 8192 498 -> 462, 128 groups x 256 rows, 3072 -> 768 119 -> 113; 64 x
 //     256, 4096 -> 1024 (three rounds) 98 -> 104, 16384 x 1024 -> 4096 81 -> 92.
+int pick_fp8_kernel(int cus, int N, int C, int KB, int Nout, bool rows8, int act)
+{
+    const auto tiles = [&](int rows, int columns) { return (long long)N * ((C + rows - 1) / rows) * ((Nout + columns - 1) / columns); };
+    if (rows8) return KB <= 4 && tiles(32, 128) <= cus ? kFp8FewRowsCodes : kFp8Ring128;
+    if (tiles(32, 32) <= 2 * cus) return kFp8FewRowsY;
+    return act == 0 && KB >= 16 && tiles(128, 256) >= 4 * cus ? kFp8Ring256 : kFp8Ring128;
+}
+
 hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s)
 {
     const bool rows8 = g.y8 || g.p8 || g.g8;
-    const auto tiles = [&](int rows, int columns) {
-        return (long long)g.N * ((g.C + rows - 1) / rows) * ((g.Nout + columns - 1) / columns);
-    };
-    if (rows8 ? g.KB <= 4 && tiles(32, 128) <= tune.cus : tiles(32, 32) <= 2 * tune.cus)
-        return rows8 ? launch_rows<4, 2, true>(g, s) : launch_rows<1, 4, false>(g, s);
+    switch (pick_fp8_kernel(tune.cus, g.N, g.C, g.KB, g.Nout, rows8, g.act)) {
+    case kFp8FewRowsY: return launch_rows<1, 4, false>(g, s);
+    case kFp8FewRowsCodes: return launch_rows<4, 2, true>(g, s);
+    case kFp8Ring256: return launch_fp8_ring<2, 1, kFp8Y, 0>(g, tune, s);
+    default: break;
+    }
     if (g.g8) return g.act == 1 ? launch_fp8_ring<1, 2, kFp8Slope, 1>(g, tune, s) : launch_fp8_ring<1, 2, kFp8Slope, 3>(g, tune, s);
-    if (rows8) return launch_act<kFp8Rows>(g, tune, s);
-    if (g.act == 0 && g.KB >= 16 && tiles(128, 256) >= 4 * tune.cus) return launch_fp8_ring<2, 1, kFp8Y, 0>(g, tune, s);
-    return launch_act<kFp8Y>(g, tune, s);
+    return rows8 ? launch_act<kFp8Rows>(g, tune, s) : launch_act<kFp8Y>(g, tune, s);
 }
 
 }  // namespace smile

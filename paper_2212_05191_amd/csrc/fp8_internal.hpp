@@ -52,6 +52,8 @@ struct Fp8Gemm {
     int row_tiles, col_tiles;
     bool backwards;                  // ring kernels: walk the tiles from the last group to the first
 };
+enum Fp8Kernel { kFp8FewRowsY, kFp8FewRowsCodes, kFp8Ring128, kFp8Ring256 };   // 32 x 32 tiles, 32 x 128; 128 x 128, 128 x 256
+int pick_fp8_kernel(int cus, int N, int C, int KB, int Nout, bool rows8, int act);   // rows8: 8-bit rows are written or read in the epilogue
 hipError_t launch_fp8_gemm(const Fp8Gemm &g, const Tuning &tune, hipStream_t s);
 hipError_t launch_fp8_near_zero(const Fp8Gemm &g, hipStream_t s);   // after a product with p8: its codes next to zero from exact sums
 
