@@ -145,6 +145,15 @@ __device__ __forceinline__ uint32_t pack_block(const float *v, u32x2 &codes)
     return byte;
 }
 
+// The activations of the products: activate's, but NaN stays NaN, which is what becomes of a row's or a column's NaN codes (ReLU by the maximum that
+// hands NaN on: one instruction)
+template <int ACT>
+__device__ __forceinline__ float fp8_activate(float v)
+{
+    if constexpr (ACT == 1) return __builtin_elementwise_maximum(v, 0.f);
+    else return activate<ACT>(v);
+}
+
 __device__ __forceinline__ int rows_of(const int32_t *rows, int e, int C) { return rows ? min(max(rows[e], 0), C) : C; }
 
 }  // namespace

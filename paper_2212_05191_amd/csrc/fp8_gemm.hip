@@ -29,10 +29,10 @@ __device__ __forceinline__ void activate8(int act, float *v)
 {
     if (act == 1) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate<1>(v[k]);
+        for (int k = 0; k < 8; ++k) v[k] = fp8_activate<1>(v[k]);
     } else if (act == 3) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate<3>(v[k]);
+        for (int k = 0; k < 8; ++k) v[k] = fp8_activate<3>(v[k]);
     }
 }
 

@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
 #pragma unroll
             for (int i = 0; i < TN; ++i)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[i][j][v] = activate<ACT>(acc[i][j][v]);
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = fp8_activate<ACT>(acc[i][j][v]);
         }
     };
     // y: rounded, staged as [32 rows][QB * 32 columns] of 16 bits (or half as many columns of fp32), stored row-contiguously

@@ -1,0 +1,74 @@
+"""What is not finite in the products of 8-bit operands: NaN stays in its row and column through the activations.  Both
+kernels, by the library's own rule.  Tolerances as in test_gpu_fp8.py."""
+import numpy as np
+import pytest
+import torch
+
+import fp8_reference as R
+from paper_2212_05191_amd import binding as B
+from test_gpu_fp8 import dev, half, host, near, packed
+
+pytestmark = pytest.mark.gpu
+
+FEW, RING = (7, 512, 256), (300, 640, 2048)      # rows, contraction, columns
+KINDS = pytest.mark.parametrize("C,K,Nout", (FEW, RING))
+
+
+def expected_kernel(C, K, Nout, rows8, act):
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    assert R.kernel_of(cus, 1, C, K, Nout, rows8, act) == ((1 if rows8 else 0) if C == FEW[0] else 2)
+
+
+def product(x8, xs, w8, wsc, K, Nout, act, y=None, y8=False, pre8=False, grad8=(None, None)):
+    """y (of the storage type `y`), (y8, its scales), (pre8, its scales) of one group"""
+    C = x8.shape[1]
+    expected_kernel(C, K, Nout, bool(y8 or pre8 or grad8[0] is not None), act)
+    out = torch.zeros((1, C, Nout), dtype=y, device="cuda:0") if y else None
+    o8, p8 = (B.alloc_fp8_rows(1, C, Nout) if want else (None, None) for want in (y8, pre8))
+    B.smile_fp8_gemm(B.make_fp8_gemm_args(x8, xs, w8, wsc, K, Nout, act=act, y=out, y8=o8[0], y_scale=o8[1], pre8=p8[0], pre_scale=p8[1],
+                                          grad8=grad8[0], grad_scale=grad8[1], dtype="bf16"))
+    return out, o8, p8
+
+
+def check_values(got, want, tol, lost, what):
+    """`lost`: where the values are NaN; the others as given"""
+    assert np.array_equal(np.isnan(got), lost), (what, int(np.isnan(got).sum()), int(lost.sum()))
+    near(np.where(lost, 0.0, got), np.where(lost, 0.0, want), tol, what)
+
+
+def check_rows8(rows8, want, slack, lost, what):
+    codes, scales = host(rows8[0]), host(rows8[1])
+    assert np.array_equal((codes[0] & 0x7f) == 0x7f, lost), (what, int(((codes[0] & 0x7f) == 0x7f).sum()), int(lost.sum()))
+    got = R.unpack_rows(codes, scales, want.shape[1])[0]
+    fine = np.where(lost, 0.0, want)
+    near(np.where(lost, 0.0, got), fine, R.row_step(fine[None], scales)[0] * (1 + 2.0 ** -10) + slack, what)
+
+
+def operands(C, K, Nout, seed):
+    r = np.random.default_rng(seed + C)
+    return r, r.standard_normal((1, C, K)), 0.05 * r.standard_normal((1, Nout, K))
+
+
+def nan_operands(C, K, Nout):
+    r, x, w = operands(C, K, Nout, 1)
+    (x8, xs), x = packed(x)
+    (w8, wsc), w = packed(w, True)
+    x8[0, 3, 100] = 0x7f
+    w8[0, 140, 7] = 0xff
+    lost = np.zeros((C, Nout), bool)
+    lost[3], lost[:, 140] = True, True
+    return r, (x8, xs, w8, wsc), x[0] @ w[0].T, max(K, 256) * 2.0 ** -23 * (np.abs(x[0]) @ np.abs(w[0]).T), lost
+
+
+@KINDS
+@pytest.mark.parametrize("act", ("relu", "gelu"))
+def test_nan_passes_through_the_activation(C, K, Nout, act):
+    _, ops, p, err, lost = nan_operands(C, K, Nout)
+    v, verr = R.act(p, act), err * 1.13 + 4e-7 * (1 + np.abs(p))
+    for y in (torch.float32, torch.bfloat16):
+        out = product(*ops, K, Nout, act, y=y)[0]
+        check_values(host(out)[0], v, verr + half(v, "f32" if y is torch.float32 else "bf16") * (1 + 2.0 ** -10), lost, y)
+    out, y8, p8 = product(*ops, K, Nout, act, y=torch.float32, y8=True, pre8=True)
+    check_values(host(out)[0], v, verr + half(v, "f32"), lost, "y beside 8 bits")
+    check_rows8(y8, v, verr, lost, "y8")
+    check_rows8(p8, p, err, lost, "pre8")
