@@ -396,7 +396,7 @@ smile_status smile_layer_backward(smile_ctx *ctx, const smile_backward_io *io, f
  * Packing: b is the least byte >= 1 for which the block's largest magnitude is at most 448 * 2^(b - 127), so
  * a block of zeros has b = 1; value / 2^(b - 127) is rounded to the nearest code, ties to even, with
  * gradual underflow.  Infinities and NaN become NaN codes and do not count for b.  Unlike those of the layer
- * these operators take NaN: it stays in its row and column, through the activations too.
+ * these operators take NaN: it stays in its row and column, through the activations too, and the derivative at a kept NaN is NaN.
  * 8-bit weights w[N][Nout][K] have one scale for each 128 x 128 block:
  *   codes  [N][Nout][smile_fp8_pitch(K)],  scales [N][ceil(K/128)][smile_fp8_scale_pitch(ceil(Nout/128))]
  * and in transposed form the same codes as [N][K][smile_fp8_pitch(Nout)] with scales

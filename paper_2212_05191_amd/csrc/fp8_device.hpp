@@ -153,6 +153,17 @@ __device__ __forceinline__ float fp8_activate(float v)
     if constexpr (ACT == 1) return __builtin_elementwise_maximum(v, 0.f);
     else return activate<ACT>(v);
 }
+// Their derivatives at a kept value; at NaN, which a kept infinity is too: NaN
+template <int ACT>
+__device__ __forceinline__ float fp8_slope(float g)
+{
+    if constexpr (ACT == 1) {
+        const float v = __builtin_elementwise_maximum(g, 0.f);
+        return v > 0.f ? 1.f : v;
+    } else {
+        return activate_grad<2>(g);
+    }
+}
 
 __device__ __forceinline__ int rows_of(const int32_t *rows, int e, int C) { return rows ? min(max(rows[e], 0), C) : C; }
 

@@ -69,10 +69,10 @@ __device__ __forceinline__ void finish8(const Fp8Gemm &a, int e, int r, int col,
             unpack4(c[1], s, g + 4);
             if (a.act == 1) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= activate_grad<1>(g[k]);
+                for (int k = 0; k < 8; ++k) v[k] *= fp8_slope<1>(g[k]);
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= activate_grad<2>(g[k]);
+                for (int k = 0; k < 8; ++k) v[k] *= fp8_slope<3>(g[k]);
             }
         } else {
             activate8(a.act, v);

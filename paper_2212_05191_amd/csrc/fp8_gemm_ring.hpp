@@ -527,7 +527,7 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
         lds_char *const largest = lds + 2 * STAGE + STAGING;
         if (KIND == kFp8Rows && a.p8) store_rows8(a.p8, a.ps, largest);
         // times the activation's derivative at the kept rows, which take the way through LDS that 8-bit rows take out
-        const auto times_slope = [&](auto post) __attribute__((always_inline)) {
+        const auto times_slope = [&](auto act) __attribute__((always_inline)) {
             for_constants<TM>([&](auto jj) {
                 constexpr int j = decltype(jj)::value;
                 if (cur.rt * BM + row_at(j) >= rows) return;
@@ -547,13 +547,13 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
                             float g[4];
                             unpack4(*(const lds_u32 *)(stg + orow * SROW8 + i * 32 + 8 * q + 4 * ohi), s, g);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) acc[H * QB + i][j][4 * q + k] *= activate_grad<decltype(post)::value>(g[k]);
+                            for (int k = 0; k < 4; ++k) acc[H * QB + i][j][4 * q + k] *= fp8_slope<decltype(act)::value>(g[k]);
                         }
                 });
             });
         };
         if constexpr (KIND == kFp8Slope) {
-            times_slope(std::integral_constant<int, ACT == 1 ? 1 : 2>{});
+            times_slope(std::integral_constant<int, ACT>{});
         } else {
             activate_all();
         }

@@ -1,4 +1,4 @@
-"""What is not finite in the products of 8-bit operands: NaN stays in its row and column through the activations.  Both
+"""What is not finite in the products of 8-bit operands: NaN stays in its row and column through the activations and their derivatives.  Both
 kernels, by the library's own rule.  Tolerances as in test_gpu_fp8.py."""
 import numpy as np
 import pytest
@@ -72,3 +72,20 @@ def test_nan_passes_through_the_activation(C, K, Nout, act):
     check_values(host(out)[0], v, verr + half(v, "f32"), lost, "y beside 8 bits")
     check_rows8(y8, v, verr, lost, "y8")
     check_rows8(p8, p, err, lost, "pre8")
+
+
+@KINDS
+@pytest.mark.parametrize("act", ("relu", "gelu"))
+def test_nan_of_a_kept_value_passes_through_the_derivative(C, K, Nout, act):
+    r, x, w = operands(C, K, Nout, 2)
+    (x8, xs), x = packed(x)
+    (w8, wsc), w = packed(w, True)
+    g8, g = packed(2.0 * r.standard_normal((1, C, Nout)))
+    g8[0][0, 2, 50], g8[0][0, C - 1, Nout - 1] = 0x7f, 0xff
+    lost = np.zeros((C, Nout), bool)
+    lost[2, 50] = lost[C - 1, Nout - 1] = True
+    p, err, slope = x[0] @ w[0].T, max(K, 256) * 2.0 ** -23 * (np.abs(x[0]) @ np.abs(w[0]).T), R.act_grad(g[0], act)
+    v, verr = p * slope, err * np.abs(slope) + np.abs(p) * 4e-7 * (1 + np.abs(g[0]))
+    out, y8, _ = product(x8, xs, w8, wsc, K, Nout, act, y=torch.float32, y8=True, grad8=g8)
+    check_values(host(out)[0], v, verr + half(v, "f32"), lost, "y")
+    check_rows8(y8, v, verr, lost, "y8")
