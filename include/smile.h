@@ -457,6 +457,7 @@ enum { SMILE_ACT_NONE = 2 };   /* smile_fp8_gemm: no activation */
  * y: v in the storage type; y8 / y_scale: v as 8-bit rows; pre8 / pre_scale: p as 8-bit rows, the checkpoint that a
  * backward product takes as grad8 (with SMILE_ACT_RELU its codes next to zero come from sums in 64 bits, since the derivative
  * goes by the side of zero).  With weights in transposed form it is the gradient of the rows.
+ * A sum that overflows is infinite, and so is its activation (that of -infinity is 0): a NaN code in 8 bits.
  * GELU is the erf form with the accuracy of the 16-bit expert FFN.  Sums are held in fp32.  The matrix cores add the
  * products of 16 neighbouring k at a time to about 2^-16 of the largest of them: normwise 1.5e-5 on normally distributed
  * values, 6e-5 where a block's codes are spread evenly over all exponents. */

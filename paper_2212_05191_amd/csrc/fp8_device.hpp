@@ -145,13 +145,14 @@ __device__ __forceinline__ uint32_t pack_block(const float *v, u32x2 &codes)
     return byte;
 }
 
-// The activations of the products: activate's, but NaN stays NaN, which is what becomes of a row's or a column's NaN codes (ReLU by the maximum that
-// hands NaN on: one instruction)
+// The activations of the products (ACT: 0 none, 1 ReLU, 3 GELU): activate's, but NaN stays NaN, which is what becomes of a row's or a column's NaN codes (ReLU
+// by the maximum that hands NaN on: one instruction), and a sum that overflowed stays infinite: as the largest finite value it would take
+// the scale of its block with it, and the other 127 values to zero
 template <int ACT>
 __device__ __forceinline__ float fp8_activate(float v)
 {
     if constexpr (ACT == 1) return __builtin_elementwise_maximum(v, 0.f);
-    else return activate<ACT>(v);
+    else return activate<ACT == 3 ? 4 : ACT>(v);
 }
 // Their derivatives at a kept value; at NaN, which a kept infinity is too: NaN
 template <int ACT>

@@ -36,13 +36,14 @@ typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
 
 constexpr int kXcds = 8;
 
-// ACT: 0 none, 1 ReLU, 2 GELU (erff; fp32 path), 3 GELU (rational erfc; 16-bit path)
+// ACT: 0 none, 1 ReLU, 2 GELU (erff; fp32 path), 3 GELU (rational erfc; 16-bit path), 4 the same, which keeps infinity (for
+// fp32 and 8-bit results)
 template <int ACT>
 __device__ __forceinline__ float activate(float v)
 {
     if constexpr (ACT == 1) return v > 0.f ? v : 0.f;
     else if constexpr (ACT == 2) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-    else if constexpr (ACT == 3) {
+    else if constexpr (ACT == 3 || ACT == 4) {
         // GELU(v) = v * Phi(v) = max(v,0) - |v| * erfc(|v|/sqrt2)/2, with erfc from the rational
         // approximation 7.1.26 of Abramowitz & Stegun (|error| < 1.5e-7, far below bf16 resolution):
         // erfc(z) = (a1 t + ... + a5 t^5) exp(-z^2), t = 1/(1 + p z).  ~15 VALU ops, no branches.  The exponential is a factor, so
@@ -61,7 +62,9 @@ __device__ __forceinline__ float activate(float v)
         const float ex = __builtin_amdgcn_exp2f(v * v * (-0.5f * 1.4426950408889634f));
         float most;   // in a scalar register: the compiler would keep it in a vector register, of which the ring kernels have none to spare
         asm("s_mov_b32 %0, 0x7f7fffff" : "=s"(most));
-        return __builtin_amdgcn_fmed3f(v, 0.f, most) - __builtin_amdgcn_fmed3f(av, 0.f, most) * (poly * t * ex);
+        float top = most;
+        if constexpr (ACT == 4) asm("s_mov_b32 %0, 0x7f800000" : "=s"(top));   // (opaque too: a literal would go into a vector register)
+        return __builtin_amdgcn_fmed3f(v, 0.f, top) - __builtin_amdgcn_fmed3f(av, 0.f, most) * (poly * t * ex);
     } else return v;
 }
 

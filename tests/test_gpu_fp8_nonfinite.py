@@ -1,5 +1,5 @@
-"""What is not finite in the products of 8-bit operands: NaN stays in its row and column through the activations and their derivatives.  Both
-kernels, by the library's own rule.  Tolerances as in test_gpu_fp8.py."""
+"""What is not finite in the products of 8-bit operands: NaN stays in its row and column through the activations and their derivatives, and a product
+that overflows keeps to its element.  Both kernels, by the library's own rule.  Tolerances as in test_gpu_fp8.py."""
 import numpy as np
 import pytest
 import torch
@@ -89,3 +89,30 @@ def test_nan_of_a_kept_value_passes_through_the_derivative(C, K, Nout, act):
     out, y8, _ = product(x8, xs, w8, wsc, K, Nout, act, y=torch.float32, y8=True, grad8=g8)
     check_values(host(out)[0], v, verr + half(v, "f32"), lost, "y")
     check_rows8(y8, v, verr, lost, "y8")
+
+
+@KINDS
+@pytest.mark.parametrize("act", ("none", "relu", "gelu"))
+def test_a_product_that_overflows_keeps_to_its_element(C, K, Nout, act):
+    """Row 3: 2^127 times 4 in column 5, times -4 in column 200; everything else is ordinary."""
+    _, x, w = operands(C, K, Nout, 3)
+    x[0, 3, :128], x[0, :, 7], w[0, :, 7] = 0.0, 0.0, 0.0
+    x[0, 3, 7], w[0, 5, 7], w[0, 200, 7] = 2.0 ** 127, 4.0, -4.0
+    (x8, xs), x = packed(x)
+    (w8, wsc), w = packed(w, True)
+    x[0, :, 7] = 0.0
+    p, err = x[0] @ w[0].T, max(K, 256) * 2.0 ** -23 * (np.abs(x[0]) @ np.abs(w[0]).T)
+    v, verr = R.act(p, act), err * 1.13 + 4e-7 * (1 + np.abs(p))
+    v[3, 5], v[3, 200] = np.inf, -np.inf if act == "none" else 0.0
+    verr[3, 5] = verr[3, 200] = 0.0
+    none = np.zeros((C, Nout), bool)
+    for y in (torch.float32, torch.bfloat16):
+        out = host(product(x8, xs, w8, wsc, K, Nout, act, y=y)[0])[0]
+        near(out, v, verr + np.where(np.isinf(v), 0.0, half(np.where(np.isinf(v), 0.0, v), "f32" if y is torch.float32 else "bf16")) * (1 + 2.0 ** -10), y)
+    out, y8, p8 = product(x8, xs, w8, wsc, K, Nout, act, y=torch.float32, y8=True, pre8=True)
+    near(host(out)[0], v, verr + half(np.where(np.isinf(v), 0.0, v), "f32"), "y beside 8 bits")
+    lost, kept = none.copy(), none.copy()
+    lost[3, 5], lost[3, 200] = True, act == "none"
+    kept[3, 5] = kept[3, 200] = True
+    check_rows8(y8, v, verr, lost, "y8")
+    check_rows8(p8, p, err, kept, "pre8")
