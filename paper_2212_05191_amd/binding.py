@@ -547,9 +547,12 @@ def smile_fp8_pack_weights(w, codes, scales, codes_t=None, scales_t=None, stream
 
 
 def smile_fp8_dispatch(ctx: Ctx, x8, x_scale, group_idx, local_idx, slot, xe8, xe_scale, stream=None):
+    import torch
     d = ctx.desc
     _check_rows8("x8", x8, x_scale, 1, d.T, d.d_model)
     _check_rows8("xe8", xe8, xe_scale, d.n_groups * d.m_local, d.capacity, d.d_model)
+    for name, t in (("group_idx", group_idx), ("local_idx", local_idx), ("slot", slot)):
+        _check_like(name, t, (d.T,), torch.int32)
     _check(load().smile_fp8_dispatch(ctx.handle, _ptr(x8), _ptr(x_scale), _ptr(group_idx), _ptr(local_idx), _ptr(slot), _ptr(xe8),
                                      _ptr(xe_scale), _stream(stream)), "smile_fp8_dispatch")
 

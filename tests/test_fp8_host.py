@@ -1,6 +1,7 @@
 """Host side of the 8-bit operators: size helpers, argument checks (which run before anything touches a GPU), the binding's
 checks of shapes and types, and the reference itself against differences.  No kernel is launched here."""
 import ctypes as C
+import types
 
 import numpy as np
 import pytest
@@ -154,6 +155,19 @@ def test_binding_checks_shapes_and_types():
         B.make_fp8_gemm_args(codes, scales, wc, wsc, 64, 96, y=torch.zeros(96, 4, dtype=bf).T)
     args = B.make_fp8_gemm_args(codes, scales, wc, wsc, 64, 96, y=torch.zeros(4, 96, dtype=bf))
     assert (args.N, args.C, args.K, args.Nout, args.dtype, args.act) == (1, 4, 64, 96, 1, 2)
+
+
+@pytest.mark.parametrize("which", (0, 1, 2))
+def test_dispatch_checks_its_indices(which):
+    """Indices of another type or fewer of them than tokens: the kernel would read beyond them, and write where they point."""
+    T = 6
+    ctx = types.SimpleNamespace(desc=B.make_desc(T, 64, 128, 2, 2, 3), handle=None)
+    for bad, error in ((torch.zeros(T, dtype=torch.int64), TypeError), (torch.zeros(T - 1, dtype=torch.int32), ValueError),
+                       (torch.zeros(T, 1, dtype=torch.int32), ValueError)):
+        index = [torch.zeros(T, dtype=torch.int32) for _ in range(3)]
+        index[which] = bad
+        with pytest.raises(error):
+            B.smile_fp8_dispatch(ctx, *B.alloc_fp8_rows(1, T, 64, "cpu"), *index, *B.alloc_fp8_rows(4, 3, 64, "cpu"))
 
 
 # ------------------------------------------------------------------ the reference
