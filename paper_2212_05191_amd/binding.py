@@ -423,6 +423,8 @@ def _has_shape(name, t, shape):
 def _check_codes(name, codes, scales, N, rows, K, scaled):
     """Codes [N][rows][K up to a multiple of 128] and scales [N][blocks of K][`scaled` up to a multiple of 16]: the shapes that
     the library takes for granted."""
+    if codes is None or scales is None:
+        raise ValueError(f"{name}: codes and scales go together")
     blocks = -(-K // 128)
     _has_shape(name, codes, (N, rows, blocks * 128))
     _has_shape(name + " scales", scales, (N, blocks, -(-scaled // 16) * 16))

@@ -170,6 +170,20 @@ def test_dispatch_checks_its_indices(which):
             B.smile_fp8_dispatch(ctx, *B.alloc_fp8_rows(1, T, 64, "cpu"), *index, *B.alloc_fp8_rows(4, 3, 64, "cpu"))
 
 
+def test_codes_without_scales_are_refused():
+    x, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.bfloat16)
+    (codes, scales), (wc, wsc) = B.alloc_fp8_rows(1, 4, 64, "cpu"), B.alloc_fp8_weights(1, 64, 64, "cpu")
+    y = torch.zeros(4, 64, dtype=torch.bfloat16)
+    for call in (lambda: B.smile_rms_norm(x, None, w, 1e-5, y8=codes), lambda: B.smile_fp8_pack_rows(x, codes, None),
+                 lambda: B.smile_fp8_pack_rows(x, None, scales), lambda: B.smile_fp8_unpack_rows(codes, None, y),
+                 lambda: B.smile_fp8_pack_weights(torch.zeros(64, 64), wc, wsc, wc),
+                 lambda: B.make_fp8_gemm_args(codes, None, wc, wsc, 64, 64, y=y), lambda: B.make_fp8_gemm_args(codes, scales, wc, None, 64, 64, y=y),
+                 lambda: B.make_fp8_gemm_args(codes, scales, wc, wsc, 64, 64, y8=codes), lambda: B.make_fp8_gemm_args(codes, scales, wc, wsc, 64, 64, y=y, pre8=codes),
+                 lambda: B.make_fp8_gemm_args(codes, scales, wc, wsc, 64, 64, act="relu", y=y, grad8=codes)):
+        with pytest.raises(ValueError):
+            call()
+
+
 # ------------------------------------------------------------------ the reference
 
 def test_reference_codes_agree_with_torch():
