@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256, OCC) void fp8_gemm_ring_kernel(Fp8Gemm a)
 
     const int S = a.KB, pitch = a.KB * kFp8Block;
     LiveTileWalk<BM> walk;
-    walk.init(a.rows, a.N, a.C, a.col_tiles, false, a.backwards);
+    walk.init(a.rows, a.N, a.C, a.col_tiles, false);
     struct Tile {
         int e, rt, ct, rows;
     };

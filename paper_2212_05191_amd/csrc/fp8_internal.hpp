@@ -50,7 +50,6 @@ struct Fp8Gemm {
     int Cs, Ws;                      // bytes of a line of scales: rows, blocks of columns
     int dtype, act;                  // act: 0 none, 1 ReLU, 3 GELU
     int row_tiles, col_tiles;
-    bool backwards;                  // ring kernels: walk the tiles from the last group to the first
 };
 enum Fp8Kernel { kFp8FewRowsY, kFp8FewRowsCodes, kFp8Ring128, kFp8Ring256 };   // 32 x 32 tiles, 32 x 128; 128 x 128, 128 x 256
 int pick_fp8_kernel(int cus, int N, int C, int KB, int Nout, bool rows8, int act);   // rows8: 8-bit rows are written or read in the epilogue
