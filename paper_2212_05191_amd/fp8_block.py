@@ -63,10 +63,10 @@ class Fp8Block:
         self.norm_ws = scratch(B.smile_rms_norm_backward_workspace_bytes(T, d))
         self.weight_ws = scratch(B.smile_fp8_weight_grad_workspace_bytes(N, cap, max(d, F), desc.dtype))
 
-    def pack_weights(self, w1, w2):
+    def pack_weights(self, w1, w2, stream=None):
         """The experts' weights to 8 bits: once for serving, after every optimizer step in training."""
         for w, packed, transposed in ((w1, self.w1, self.w1t), (w2, self.w2, self.w2t)):
-            B.smile_fp8_pack_weights(w, *packed, *(transposed or (None, None)))
+            B.smile_fp8_pack_weights(w, *packed, *(transposed or (None, None)), stream=stream)
 
     def forward(self, x, residual, stream=None):
         """x, residual [T, d] -> (s, y): the residual stream after the addition, and what the block adds to it next."""

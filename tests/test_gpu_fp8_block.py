@@ -113,3 +113,27 @@ def test_serving_block_keeps_nothing_for_a_backward_pass_and_gives_the_same_y():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
     train.close()
     serve.close()
+
+
+def test_weights_are_packed_on_the_stream_that_the_step_takes():
+    """A step as a program takes it whose work goes to a stream of its own by handle: the new weights are packed there, in front of the forward pass
+    that reads them."""
+    desc = B.make_desc(64, 128, 256, 2, 2, 32, "bf16", "gelu")
+    g = torch.Generator(device="cuda:0").manual_seed(9)
+    normal = lambda *shape: (0.05 * torch.randn(*shape, device="cuda:0", generator=g)).bfloat16()      # noqa: E731
+    x, res, nw, wi, wq = normal(64, 128) * 20, normal(64, 128) * 20, normal(128) + 1, normal(2, 128), normal(2, 128)
+    w1, w2, new1, new2 = normal(4, 256, 128), normal(4, 128, 256), normal(4, 256, 128), normal(4, 128, 256)
+    want = Fp8Block(desc, nw, wi, wq, new1, new2)
+    expect = want.forward(x, res)[1].clone()
+    block = Fp8Block(desc, nw, wi, wq, w1, w2)
+    assert not torch.equal(block.forward(x, res)[1], expect)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    block.pack_weights(new1, new2, stream=side)
+    _, y = block.forward(x, res, stream=side)
+    side.synchronize()
+    assert torch.equal(y, expect)
+    for a, b in ((block.w1t, want.w1t), (block.w2t, want.w2t)):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    want.close()
+    block.close()
