@@ -137,3 +137,31 @@ def test_weights_are_packed_on_the_stream_that_the_step_takes():
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
     want.close()
     block.close()
+
+
+def test_a_stack_of_blocks_shares_its_scratch_memory():
+    """Two blocks, the second on what the first returns: gradients with one scratch memory for both are those with two, and a block
+    with a shared one allocates none."""
+    desc = B.make_desc(200, 128, 256, 2, 2, 60, "bf16", "gelu")
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    normal = lambda *shape: (0.05 * torch.randn(*shape, device="cuda:0", generator=g)).bfloat16()      # noqa: E731
+    x, res, dy = normal(200, 128) * 20, normal(200, 128) * 20, normal(200, 128) * 20
+    weights = [(normal(128) + 1, normal(2, 128), normal(2, 128), normal(4, 256, 128), normal(4, 128, 256)) for _ in range(2)]
+
+    def gradients(share):
+        first = Fp8Block(desc, *weights[0])
+        second = Fp8Block(desc, *weights[1], scratch=first.scratch if share else None)
+        assert (second.scratch is first.scratch) == share
+        with pytest.raises(ValueError):
+            Fp8Block(B.make_desc(201, 128, 256, 2, 2, 60, "bf16", "gelu"), *weights[1], scratch=first.scratch)
+        s, y = first.forward(x, res)
+        second.forward(y, s)
+        ds = second.backward(dy)              # the gradient of y and of s alike
+        first.backward(ds, dsum=ds)
+        torch.cuda.synchronize()
+        out = [t.clone() for b in (first, second) for t in (b.ds, b.dnorm, b.bwd.dw1, b.bwd.dw2, b.bwd.dw_inter, b.bwd.dw_intra)]
+        first.close()
+        second.close()
+        return out
+
+    assert all(torch.equal(a, b) and bool(a.abs().sum() > 0) for a, b in zip(gradients(True), gradients(False)))
