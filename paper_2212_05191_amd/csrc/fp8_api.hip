@@ -212,8 +212,9 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
     // kernels of the expert FFN.
     hipError_t err = launch_fp8_unpack_rows(dtype, RowsIo{N, C, K, rows}, static_cast<const uint8_t *>(x8), static_cast<const uint8_t *>(x_scale), workspace, s);
     if (err != hipSuccess) return from_hip(err);
-    // Row counts that the device knows: buffers are made a quarter larger than what they expect (capacity factor 1.25).  The rules of the gradient
-    // kernels go by it: 64 groups of 256 rows in buffers of 320, 1024 x 4096: 280 -> 266 us.
+    // Row counts that the device knows alone: the rules of the gradient kernels, which go by the rows expected, are given four fifths of the buffers
+    // (capacity factor 1.25).  Half precision, 64 groups of 256 rows, 1024 x 4096: buffers of 320 252 -> 241 us; of 256 and of 512 rows the same either way (226,
+    // 267), as are 16 groups of 512 rows in 512 or 640, 15 of 334 in 417 and 128 of 20 in 26.
     const int tokens = rows ? (int)std::max(1ll, (long long)N * C * 4 / 5) : 0;
     const long long sx = (long long)C * Nout, sw = (long long)C * K, sy = (long long)Nout * K;
     if (is_half(dtype)) {

@@ -6,7 +6,7 @@
 //   * a lane reads its rows' bytes together with A0 and hands them to the instruction, which multiplies them in.
 // What bounds it: the latency of the units, 2 us under load, against 7 of 8 slots in flight (112 KB a CU with two workgroups, 84 KB with one of 128 x
 // 256), and the epilogue, which adds to it: 64 groups x 256 rows, 1024 -> 4096, GELU and 8-bit rows: 81 us without an epilogue, 118 without its
-// stores, 131 in all (1.05 PFLOP/s; the weights' way from HBM is 52).  Per slab 128 x 128 moves 64 KB through L2 for 1024 matrix
+// stores, 131 in all (1.05 PFLOP/s; its bytes take 68, 52 of them the weights).  Per slab 128 x 128 moves 64 KB through L2 for 1024 matrix
 // cycles of a CU, two workgroups side by side; 8192 x 8192 x 8192 2.2 PFLOP/s (2.4 in tiles of 128 x 256; a library product 2.9, at the 1.6 GHz
 // that the power limit leaves).  Tried and taken back: the epilogue in slices beside the next tile's phases from a second set of accumulators
 // (no gain: one wave issues a vector instruction every 5.5 cycles), 256 x 256 tiles (spill), requests into L2 a tile ahead (slower).

@@ -160,7 +160,8 @@ __global__ __launch_bounds__(256, 3) void fp8_weight_grad_kernel(Fp8WeightGrad a
 // The rows of a tile go through one workgroup, one slab after another (0.6 us each), while the 16-bit kernels take smaller tiles or split the rows,
 // after a widening that takes at least 8 us.  Measured, this kernel against that (us): 67 tiles of 97 rows 7 : 9, 128 of 500 16 : 21, 288 of 1000
 // 33 : 35, 576 of 512 42 : 62, 8192 of 256 173 : 238; the other way 8 tiles of 500 14.6 : 10.9, 144 of 1000 27 : 26, 256 of 2000 50 : 47, 256 of
-// 4000 89 : 83, 128 of 8192 164 : 90.
+// 4000 89 : 83, 128 of 8192 164 : 90.  From two tiles a CU on, long rows too: 1024 tiles of 3000 rows 193 : 262, of 6000 366 : 500, 1300 of 8192 655 : 730,
+// 1440 of 2048 177 : 268, 1536 of 4096 380 : 565.
 bool fp8_weight_grad_applies(int dtype, int N, int C, int Nout, int K, const Tuning &tune)
 {
     const long long tiles = (long long)N * ((Nout + kTileO - 1) / kTileO) * ((K + kTileK - 1) / kTileK);

@@ -228,9 +228,14 @@ __global__ __launch_bounds__(1024) void rms_norm_dweight_kernel(const float *__r
     }
 }
 
-// Workgroups at most, each of consecutive rows: four a CU forward, three backward, whose registers leave no room for a fourth and whose number is that
-// of the parts of dw.  us, 65536 x 1024 bf16, y alone: 768 116, 1024 103, 1280 111, 2048 108 (a copy of its bytes: 104); y8 alone 105, 92, 100, 98
+// Workgroups at most, each of consecutive rows: four a CU forward, three backward, whose number is that of the parts of dw.  That many are resident with
+// one or two pieces a lane in 16 bits (88 and 140 registers), which they were measured with.  Of four pieces (1032 to 2048 and 4104 to 8192 columns: 138 and 250
+// registers) three and two are, of eight two and one; fp32 backward: two of two pieces, one beyond.  Those run in more than one round.
+// Part of a row is in accumulation registers in backward beyond 8192 columns, in fp32 beyond 1024, where 16384 columns spill too.  us, 65536 x 1024 bf16, y alone: 768 116, 1024 103, 1280 111, 2048 108 (a copy of its bytes: 104); y8 alone 105, 92, 100, 98
 // (91); backward 512 114, 768 113, 1024 113, 4096 118 (104); 16384 x 1024: 28.3, 25.9, 27.3, 36.4 (26.0); 5003 x 960 fp16 12.4, 11.9, 11.9, 15.2 (7.4).
+// Wide rows as they are (y and sum; backward; a copy of either's bytes): bf16 8192 x 1600 21, 27 (20), 65536 x 1600 230, 177 (163), 65536 x 2048 256, 224 (208),
+// 16384 x 4096 108, 116 (104), 16384 x 8192 261, 242 (208), 4096 x 16384 122, 143 (104); fp32 65536 x 1024 219, 217 (208), 65536 x 1600 383, 335 (325),
+// 16384 x 4096 213, 226 (208), 4096 x 16384 224, 314 (208).
 constexpr int kForwardBlocks = 1024, kGradBlocks = 768;
 
 struct NormShape {
