@@ -4,7 +4,8 @@
 // of a row's typical sum (fp8_gemm.hip), which moves about four elements in a million over that border, and each of them gives
 // or takes a whole term of the gradients: with few rows in a group that is a good part of a weight's gradient.  So every code whose magnitude is below
 // 2^-5, where the largest is up to 448 (exponent field 0 or 1: three in ten thousand of normally distributed sums, several times the error) is replaced by the code of the sum in 64 bits, where
-// the products of codes and their sums are exact for all that matters.
+// the products of codes and their sums are exact for all that matters.  (The error goes by the terms.  Of 25 million sums of 768 none was left on the wrong side
+// where they cancel to a tenth of what their terms would give at random, half of one in a million at a twentieth, a tenth of one with channels 30 times the others.)
 //
 // One wave reads 1024 codes of a row, 16 a lane, and takes the near ones in turn, all lanes along the contraction.  What bounds it are the
 // waves that meet several: 3 us each, the latency of two rows and of the sum.  16 groups of 512 rows, 3072 columns, K = 768: 14 us after the
