@@ -481,7 +481,8 @@ smile_status smile_fp8_gemm(const smile_fp8_gemm_args *args, void *stream);
 
 /* Weight gradient from an operand kept in 8 bits: dw[e,o,k] = sum_{r < rows[e]} dy[e,r,o] * x[e,r,k], dy[N][C][Nout] and
  * dw[N][Nout][K] in `dtype`, x8 / x_scale 8-bit rows [N][C][K].  Products of 16-bit values (K and Nout % 64 == 0) or of fp32 ones,
- * summed in fp32 and rounded once; a group without rows gets zeros.  workspace: at least smile_fp8_weight_grad_workspace_bytes
+ * summed in fp32 and rounded once (in half precision the operand counts as what it holds: beyond +-65504 as that, below 2^-14 as
+ * its subnormals); a group without rows gets zeros.  workspace: at least smile_fp8_weight_grad_workspace_bytes
  * bytes, 256-byte aligned (the operand in `dtype`). */
 smile_status smile_fp8_weight_grad_workspace_bytes(int32_t N, int32_t C, int32_t K, int32_t dtype, size_t *bytes);
 smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K, int32_t dtype, const void *dy, const void *x8,
