@@ -6,7 +6,7 @@ import torch
 
 import fp8_reference as R
 from paper_2212_05191_amd import binding as B
-from test_gpu_fp8 import dev, half, host, near, packed
+from test_gpu_fp8 import half, host, near, packed
 
 pytestmark = pytest.mark.gpu
 
