@@ -489,6 +489,134 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
                                    const void *x_scale, const int32_t *rows, void *dw, void *workspace, size_t workspace_bytes,
                                    void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a layer without dropped tokens, and of its optimizer: k experts for a token, the (token, choice) pairs sorted by expert,
+ * products of each expert's rows (or of dense rows), the weighted return, the gradients, and an AdamW step.  They need no ctx and
+ * allocate nothing.  Workspaces are the caller's, 256-byte aligned, and only used during the call's enqueued work; calls that overlap must not share
+ * one.  The functions ending in _bytes, and smile_adamw_plan, work on the host alone.
+ * Limits: T, rows, N, k, d, K, F >= 1; N <= 4096; k <= N and k <= 64; T*k < 2^26, rows and R <= 2^27; d, K, F % 8 == 0; d <= 16384,
+ * K, F <= 32768; elements of any tensor below 2^40.
+ * Indices and row numbers are never followed outside their tensors: a pair whose expert is not in 0 .. N - 1 has no row, a row number that is not in
+ * 0 .. R - 1 counts as none, and first rows are taken as what lies in order within 0 .. rows.
+ * ------------------------------------------------------------------------- */
+
+/* k experts for each of T tokens.  v[t,e] = logits[t,e] + bias[e] (one fp32 addition; bias NULL: none), -infinity where bias[e] is: such an
+ * expert is shut off.  p[t,:] = softmax of v[t,:] (zeros if every v is -infinity).
+ *   idx[t,j]     the expert of the j-th largest v, equal ones in the order of their index; -1 where only -infinity is left
+ *   weight[t,j]  p of it, divided by the sum over the token's choices if `normalize`; 0 where idx is -1
+ *   p_sum[e]     sum over t of p[t,e], in a fixed order (fp32 over the tokens of a workgroup's lane, their sums in 64 bits); may be NULL
+ * logits[T,N], bias[N], weight[T,k], p_sum[N] fp32, idx[T,k] int32.  A NaN or +infinity among a token's v makes its weights, and p_sum, NaN.
+ * workspace: smile_topk_workspace_bytes bytes; not needed without p_sum. */
+smile_status smile_topk_workspace_bytes(int32_t T, int32_t N, size_t *bytes);
+smile_status smile_topk(int32_t T, int32_t N, int32_t k, int32_t normalize, const float *logits, const float *bias, int32_t *idx, float *weight,
+                        float *p_sum, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradient of the logits, for L = sum dweight * weight + coef * sum_e count[e] * p_sum[e] with idx and count held constant.  With u[t,e] =
+ * coef * count[e] (count NULL: 0):
+ *   not normalize:  u[t,e] += dweight[t,j] for e = idx[t,j];   dlogits = p (u - sum_e p u)
+ *   normalize:      the same without dweight, and + w (dweight[t,j] - sum_j w dweight[t,:]) at e = idx[t,j], w the weights
+ * idx as smile_topk gave it (a token's experts differ).  coef = alpha * N / (k T^2) makes the second term
+ * alpha N sum_e f_e P_e, Eq. 4 of one level with the fractions f_e = count[e] / (k T) and P_e = p_sum[e] / T.
+ * dlogits[T,N] fp32; the sum of it over t is the gradient of the bias. */
+smile_status smile_topk_backward(int32_t T, int32_t N, int32_t k, int32_t normalize, const float *logits, const float *bias, const int32_t *idx,
+                                 const float *dweight, const int32_t *count, float coef, float *dlogits, void *stream);
+
+/* The pairs (t, j), numbered t*k + j, sorted by expert idx[t,j] and then by their number:
+ *   count[e]   pairs of expert e;   start[e] = sum of count[0 .. e-1], start[N] their number
+ *   pos[t,j]   the pair's row in the sorted order, -1 without one;   source[r]  the pair of row r, -1 from start[N] to T*k - 1
+ * All int32: idx[T,k], count[N], start[N+1], pos[T,k], source[T*k]. */
+smile_status smile_sort_experts_workspace_bytes(int32_t T, int32_t k, int32_t N, size_t *bytes);
+smile_status smile_sort_experts(int32_t T, int32_t k, int32_t N, const int32_t *idx, int32_t *count, int32_t *start, int32_t *pos, int32_t *source,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Tokens to their sorted rows: xs[pos[t,j],:] = x[t,:].  x[T,d], xs[R,d] in `dtype`; rows no pair has are left as they were. */
+smile_status smile_sorted_dispatch(int32_t T, int32_t k, int32_t d, int32_t R, int32_t dtype, const void *x, const int32_t *pos, void *xs, void *stream);
+
+/* And back: y[t,:] = residual[t,:] + sum_j weight[t,j] * ys[pos[t,j],:], in fp32, rounded once.  weight NULL: ones, which makes it the gradient of
+ * smile_sorted_dispatch; residual NULL: zeros; y may be residual.  Pairs without a row add nothing.  y[T,d], ys[R,d], residual[T,d] in `dtype`. */
+smile_status smile_sorted_combine(int32_t T, int32_t k, int32_t d, int32_t R, int32_t dtype, const void *ys, const int32_t *pos, const float *weight,
+                                  const void *residual, void *y, void *stream);
+
+/* Its gradients: dys[pos[t,j],:] = weight[t,j] * dy[t,:], dweight[t,j] = sum_c dy[t,c] * ys[pos[t,j],c] (fp32; 0 for a pair without a row).
+ * Rows of dys no pair has are left as they were.  dys must not overlap dy or ys.  dweight and ys may be NULL together. */
+smile_status smile_sorted_combine_backward(int32_t T, int32_t k, int32_t d, int32_t R, int32_t dtype, const void *dy, const void *ys, const int32_t *pos,
+                                           const float *weight, void *dys, float *dweight, void *stream);
+
+/* y[r,f] = act(sum_k x[r,k] * w[e,f,k] + bias[e,f]) + residual[r,f] for the rows start[e] <= r < start[e+1] of every group e; start NULL: N = 1 and
+ * all rows.  Rows of no group are neither read nor written.  Sums, activation and the residual's addition in fp32, rounded once; `pre`, if
+ * given, receives the activation's argument (the form that smile_linear_backward reads).  act: SMILE_ACT_RELU, _GELU (erf form; 16-bit types with
+ * an error of 4e-7 (1 + |v|)) or _NONE.  y may be residual.  NaN and infinities stay in their row and column. */
+typedef struct smile_linear_args {
+    int32_t N, rows, K, F;       /* groups; rows of x, y, residual and pre; columns of x; columns of y */
+    int32_t dtype, act;
+    const void *x;               /* [rows][K] */
+    const void *w;               /* [N][F][K] */
+    const void *bias;            /* [N][F] or NULL */
+    const void *residual;        /* [rows][F] or NULL */
+    const int32_t *start;        /* [N+1] or NULL */
+    void *y;                     /* [rows][F] */
+    void *pre;                   /* [rows][F] or NULL */
+} smile_linear_args;
+smile_status smile_linear(const smile_linear_args *args, void *stream);
+
+/* Its gradients (that of the residual is dy).  With g = dy * act'(pre), rounded to the storage type where it enters a product:
+ *   dx[r,:] = sum_f g[r,f] * w[e,f,:],   dw[e,f,:] = sum_r g[r,f] * x[r,:],   dbias[e,f] = sum_r g[r,f]   (g before its rounding)
+ * summed in fp32 in a fixed order, rounded once.  Each of dx, dw, dbias may be NULL, but not all; w is needed for dx, x for dw, pre for
+ * an activation.  Rows of no group are neither read nor written; a group without rows gets zeros. */
+typedef struct smile_linear_backward_args {
+    int32_t N, rows, K, F;
+    int32_t dtype, act;
+    const void *dy;              /* [rows][F] */
+    const void *x, *w, *pre;
+    const int32_t *start;
+    void *dx;                    /* [rows][K] or NULL */
+    void *dw;                    /* [N][F][K] or NULL */
+    void *dbias;                 /* [N][F] or NULL */
+} smile_linear_backward_args;
+smile_status smile_linear_backward_workspace_bytes(const smile_linear_backward_args *args, size_t *bytes);
+smile_status smile_linear_backward(const smile_linear_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* AdamW over any number of tensors in one launch, in place.  t = step[0] + 1, g the gradient, p the master weight where there is one, else the parameter:
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr (weight_decay p + m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps));   param = p rounded;   step[0] = t
+ * in fp32 (the powers in 64 bits).  lr[1] fp32 and step[1] int32 (>= 0) are on the device, so that a captured graph follows them.
+ * State of 32 bits: m[n], v[n] fp32.  State of 8 bits: blocks of 128 neighbouring elements share a power of two, kept as its byte b:
+ *   m: e4m3 codes times 2^(b - 127), b the least byte >= 1 for which the block's largest magnitude is at most 448 * 2^(b - 127)
+ *   v: codes c of 5 exponent and 3 fraction bits without a sign, (1 + (c & 7) / 8) * 2^((c >> 3) - 30) * 2^(b - 127), 0 for c = 0; b is the power of two
+ *      of the block's largest value (at least 1); what is not 0 is at least c = 1
+ * The stored moments (not those of this step's update) are rounded up or down by 16 random bits R each: up where the part cut off is at least
+ * 1 - R / 65536 of a step.  The bits are a hash of (seed, t, tensor, element), so a step gives the same bits wherever it runs.
+ * m, v [n up to a multiple of 128], m_scale, v_scale [their blocks]; padding gets zero codes; all zeros is a new state.  A gradient that is not finite makes
+ * its parameter and first moment NaN, its v the largest code, and does not count for the block's power of two.
+ * A state that decayed below fp32's normal range is kept as far as the codes reach.
+ * The tensors of a plan share their types; each pointer is 16-byte aligned, the scales' excepted.  The plan is built on the host and copied to the device by the
+ * caller (the device copy 256-byte aligned; the step keeps a counter in it, so steps of one plan must not overlap). */
+typedef struct smile_adamw_tensor {
+    void *param;                 /* [n] in `dtype` */
+    const void *grad;            /* [n] in `grad_dtype` */
+    float *master;               /* [n] or NULL (all tensors of a plan alike); 16-bit parameters only */
+    void *m, *v;
+    void *m_scale, *v_scale;     /* 8-bit states, else NULL */
+    int64_t n;                   /* 1 .. 2^32 */
+    float weight_decay;
+} smile_adamw_tensor;
+typedef struct smile_adamw_args {
+    int32_t tensors;
+    int32_t dtype, grad_dtype;   /* of the parameters; of the gradients: the same or SMILE_DTYPE_F32 */
+    int32_t state_bits;          /* 32 or 8 */
+    int32_t has_master;
+    int32_t seed;
+    double beta1, beta2, eps;    /* 0 <= beta < 1, 0 < eps <= 1; 1 - beta is taken in 64 bits */
+    int64_t chunks;              /* filled in by smile_adamw_plan */
+} smile_adamw_args;
+smile_status smile_adamw_plan_bytes(const smile_adamw_args *args, const smile_adamw_tensor *tensors, size_t *bytes);
+smile_status smile_adamw_plan(smile_adamw_args *args, const smile_adamw_tensor *tensors, void *plan, size_t plan_bytes);
+smile_status smile_adamw(const smile_adamw_args *args, void *device_plan, size_t plan_bytes, const float *lr, int32_t *step, void *stream);
+
+/* 8-bit states of n elements (a multiple of 128) as values in `dtype` (fp32 or bfloat16), for checkpoints and inspection. */
+smile_status smile_adamw_unpack_states(int64_t n, int32_t dtype, const void *m, const void *m_scale, const void *v, const void *v_scale, void *m_value,
+                                       void *v_value, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

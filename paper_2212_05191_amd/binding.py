@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libsmile.so")
 _lib = None
 
 DTYPE = {"f32": 0, "bf16": 1, "f16": 2}
-ACT = {"relu": 0, "gelu": 1, "none": 2}   # "none": products of 8-bit operands only
+ACT = {"relu": 0, "gelu": 1, "none": 2}   # "none": products of 8-bit operands and of sorted or dense rows only
 
 OK, INVALID_ARG, BAD_SHAPE, UNSUPPORTED, WORKSPACE, HIP_ERROR = range(6)
 
@@ -53,6 +53,25 @@ class Fp8GemmArgs(C.Structure):
         "x8", "x_scale", "w8", "w_scale", "bias", "rows", "y", "y8", "y_scale", "pre8", "pre_scale", "grad8", "grad_scale")]
 
 
+class LinearArgs(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("N", "rows", "K", "F", "dtype", "act")] + [(k, C.c_void_p) for k in (
+        "x", "w", "bias", "residual", "start", "y", "pre")]
+
+
+class LinearBackwardArgs(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("N", "rows", "K", "F", "dtype", "act")] + [(k, C.c_void_p) for k in (
+        "dy", "x", "w", "pre", "start", "dx", "dw", "dbias")]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")] + [("n", C.c_int64), ("weight_decay", C.c_float)]
+
+
+class AdamWArgs(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("tensors", "dtype", "grad_dtype", "state_bits", "has_master", "seed")] + [
+        (k, C.c_double) for k in ("beta1", "beta2", "eps")] + [("chunks", C.c_int64)]
+
+
 EXPORTS = (
     "smile_status_string", "smile_version", "smile_capacity", "smile_validate_desc", "smile_workspace_bytes",
     "smile_create", "smile_create_with_workspace", "smile_destroy", "smile_gate_logits", "smile_route_bilevel",
@@ -63,6 +82,10 @@ EXPORTS = (
     "smile_fp8_pitch", "smile_fp8_scale_pitch", "smile_rms_norm", "smile_rms_norm_backward_workspace_bytes",
     "smile_rms_norm_backward", "smile_fp8_pack_rows", "smile_fp8_unpack_rows", "smile_fp8_pack_weights",
     "smile_fp8_dispatch", "smile_fp8_gemm", "smile_fp8_weight_grad_workspace_bytes", "smile_fp8_weight_grad",
+    "smile_topk_workspace_bytes", "smile_topk", "smile_topk_backward", "smile_sort_experts_workspace_bytes", "smile_sort_experts",
+    "smile_sorted_dispatch", "smile_sorted_combine", "smile_sorted_combine_backward", "smile_linear",
+    "smile_linear_backward_workspace_bytes", "smile_linear_backward", "smile_adamw_plan_bytes", "smile_adamw_plan", "smile_adamw",
+    "smile_adamw_unpack_states",
 )
 
 
@@ -123,6 +146,22 @@ def load() -> C.CDLL:
     lib.smile_fp8_gemm.argtypes = [C.POINTER(Fp8GemmArgs), vp]
     lib.smile_fp8_weight_grad_workspace_bytes.argtypes = [i32] * 4 + [sz]
     lib.smile_fp8_weight_grad.argtypes = [i32] * 5 + [vp] * 6 + [C.c_size_t, vp]
+    size = C.c_size_t
+    lib.smile_topk_workspace_bytes.argtypes = [i32, i32, sz]
+    lib.smile_topk.argtypes = [i32] * 4 + [vp] * 6 + [size, vp]
+    lib.smile_topk_backward.argtypes = [i32] * 4 + [vp] * 5 + [C.c_float, vp, vp]
+    lib.smile_sort_experts_workspace_bytes.argtypes = [i32] * 3 + [sz]
+    lib.smile_sort_experts.argtypes = [i32] * 3 + [vp] * 6 + [size, vp]
+    lib.smile_sorted_dispatch.argtypes = [i32] * 5 + [vp] * 4
+    lib.smile_sorted_combine.argtypes = [i32] * 5 + [vp] * 6
+    lib.smile_sorted_combine_backward.argtypes = [i32] * 5 + [vp] * 7
+    lib.smile_linear.argtypes = [C.POINTER(LinearArgs), vp]
+    lib.smile_linear_backward_workspace_bytes.argtypes = [C.POINTER(LinearBackwardArgs), sz]
+    lib.smile_linear_backward.argtypes = [C.POINTER(LinearBackwardArgs), vp, size, vp]
+    lib.smile_adamw_plan_bytes.argtypes = [C.POINTER(AdamWArgs), C.POINTER(AdamWTensor), sz]
+    lib.smile_adamw_plan.argtypes = [C.POINTER(AdamWArgs), C.POINTER(AdamWTensor), vp, size]
+    lib.smile_adamw.argtypes = [C.POINTER(AdamWArgs), vp, size, vp, vp, vp]
+    lib.smile_adamw_unpack_states.argtypes = [C.c_int64, i32] + [vp] * 7
     for name in EXPORTS[3:]:
         getattr(lib, name).restype = i32
     lib.smile_kernel_timing_name.restype = C.c_char_p
@@ -611,6 +650,256 @@ def smile_fp8_weight_grad(dy, x8, x_scale, dw, workspace, rows=None, stream=None
     _check(load().smile_fp8_weight_grad(N, cap, Nout, K, _dtype_code(dy), _ptr(dy), _ptr(x8), _ptr(x_scale), _ptr(rows), _ptr(dw),
                                         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
            "smile_fp8_weight_grad")
+
+
+# ------------------------------------------------------------------ a layer without dropped tokens, and its optimizer
+
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _i32():
+    import torch
+    return torch.int32
+
+
+def _check_device(*tensors):
+    """Tensors of the current device: a kernel would follow any other pointer blindly."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def smile_topk_workspace_bytes(T, N) -> int:
+    out = C.c_size_t(0)
+    _check(load().smile_topk_workspace_bytes(int(T), int(N), C.byref(out)), "smile_topk_workspace_bytes")
+    return int(out.value)
+
+
+def smile_topk(logits, idx, weight, bias=None, normalize=False, p_sum=None, workspace=None, stream=None):
+    """logits[T, N] -> the k experts idx[T, k] of each token, their weights, and the column sums of the probabilities."""
+    T, N = logits.shape
+    k = idx.shape[-1]
+    f32 = _f32()
+    _check_like("logits", logits, (T, N), f32)
+    _check_like("idx", idx, (T, k), _i32())
+    _check_like("weight", weight, (T, k), f32)
+    _check_like("bias", bias, (N,), f32)
+    _check_like("p_sum", p_sum, (N,), f32)
+    _check_device(logits, idx, weight, bias, p_sum, workspace)
+    _check(load().smile_topk(T, N, k, int(bool(normalize)), _ptr(logits), _ptr(bias), _ptr(idx), _ptr(weight), _ptr(p_sum), _ptr(workspace),
+                             _nbytes(workspace), _stream(stream)), "smile_topk")
+
+
+def smile_topk_backward(logits, idx, dweight, dlogits, bias=None, normalize=False, count=None, coef=0.0, stream=None):
+    """Gradient of the logits from that of the weights and coef * count for each column of p_sum."""
+    T, N = logits.shape
+    k = idx.shape[-1]
+    f32 = _f32()
+    _check_like("logits", logits, (T, N), f32)
+    _check_like("idx", idx, (T, k), _i32())
+    _check_like("dweight", dweight, (T, k), f32)
+    _check_like("dlogits", dlogits, (T, N), f32)
+    _check_like("bias", bias, (N,), f32)
+    _check_like("count", count, (N,), _i32())
+    _check_device(logits, idx, dweight, dlogits, bias, count)
+    _check(load().smile_topk_backward(T, N, k, int(bool(normalize)), _ptr(logits), _ptr(bias), _ptr(idx), _ptr(dweight), _ptr(count), float(coef),
+                                      _ptr(dlogits), _stream(stream)), "smile_topk_backward")
+
+
+def smile_sort_experts_workspace_bytes(T, k, N) -> int:
+    out = C.c_size_t(0)
+    _check(load().smile_sort_experts_workspace_bytes(int(T), int(k), int(N), C.byref(out)), "smile_sort_experts_workspace_bytes")
+    return int(out.value)
+
+
+def smile_sort_experts(idx, count, start, pos, source, workspace=None, stream=None):
+    """The pairs of idx[T, k] sorted by expert: count[N], start[N + 1], pos[T, k] (the pair's row or -1), source[T * k] (the row's pair or -1)."""
+    T, k = idx.shape
+    N, i32 = count.shape[0], _i32()
+    for name, t, shape in (("idx", idx, (T, k)), ("count", count, (N,)), ("start", start, (N + 1,)), ("pos", pos, (T, k)), ("source", source, (T * k,))):
+        _check_like(name, t, shape, i32)
+    _check_device(idx, count, start, pos, source, workspace)
+    _check(load().smile_sort_experts(T, k, N, _ptr(idx), _ptr(count), _ptr(start), _ptr(pos), _ptr(source), _ptr(workspace), _nbytes(workspace),
+                                     _stream(stream)), "smile_sort_experts")
+
+
+def _check_pairs(pos, T, weight=None, dweight=None):
+    k = pos.shape[-1]
+    _check_like("pos", pos, (T, k), _i32())
+    _check_like("weight", weight, (T, k), _f32())
+    _check_like("dweight", dweight, (T, k), _f32())
+    return k
+
+
+def smile_sorted_dispatch(x, pos, xs, stream=None):
+    """Row t of x[T, d] to the rows pos[t, :] of xs[R, d]."""
+    T, d = x.shape
+    k, R = _check_pairs(pos, T), xs.shape[0]
+    _check_like("xs", xs, (R, d), x.dtype)
+    _check_device(x, pos, xs)
+    _check(load().smile_sorted_dispatch(T, k, d, R, _dtype_code(x), _ptr(x), _ptr(pos), _ptr(xs), _stream(stream)), "smile_sorted_dispatch")
+
+
+def smile_sorted_combine(ys, pos, y, weight=None, residual=None, stream=None):
+    """y[T, d] = residual + the weighted sum of each token's rows of ys[R, d]."""
+    (R, d), T = ys.shape, pos.shape[0]
+    k = _check_pairs(pos, T, weight)
+    _check_like("y", y, (T, d), ys.dtype)
+    _check_like("residual", residual, (T, d), ys.dtype)
+    _check_device(ys, pos, y, weight, residual)
+    _check(load().smile_sorted_combine(T, k, d, R, _dtype_code(ys), _ptr(ys), _ptr(pos), _ptr(weight), _ptr(residual), _ptr(y), _stream(stream)),
+           "smile_sorted_combine")
+
+
+def smile_sorted_combine_backward(dy, ys, pos, weight, dys, dweight, stream=None):
+    """Gradients of smile_sorted_combine: dys[R, d] and dweight[T, k] (ys and dweight None: without the latter)."""
+    (T, d), R = dy.shape, dys.shape[0]
+    k = _check_pairs(pos, T, weight, dweight)
+    _check_like("ys", ys, (R, d), dy.dtype)
+    _check_like("dys", dys, (R, d), dy.dtype)
+    _check_device(dy, ys, pos, weight, dys, dweight)
+    _check(load().smile_sorted_combine_backward(T, k, d, R, _dtype_code(dy), _ptr(dy), _ptr(ys), _ptr(pos), _ptr(weight), _ptr(dys), _ptr(dweight),
+                                                _stream(stream)), "smile_sorted_combine_backward")
+
+
+def _linear_shapes(x, w, start):
+    rows, K = x.shape
+    N, F = _grouped(w)[:2]
+    if _grouped(w)[2] != K:
+        raise ValueError(f"w has shape {tuple(w.shape)}, not {(N, F, K)}")
+    if start is not None:
+        _check_like("start", start, (N + 1,), _i32())
+    return N, rows, K, F
+
+
+def _like_grouped(name, t, shape, dtype):
+    """t of a shape that may leave out a first extent of 1"""
+    if t is not None and tuple(t.shape) != shape and not (shape[0] == 1 and tuple(t.shape) == shape[1:]):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {shape}")
+    if t is not None and t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+
+
+def make_linear_args(x, w, y, bias=None, act="none", residual=None, start=None, pre=None) -> LinearArgs:
+    """The argument block of smile_linear: x[rows, K], w[N, F, K] (or [F, K]), y[rows, F], bias[N, F], residual and pre like y, start[N + 1].  The block
+    keeps the tensors alive."""
+    N, rows, K, F = _linear_shapes(x, w, start)
+    dtype = x.dtype
+    _like_grouped("w", w, (N, F, K), dtype)
+    _like_grouped("bias", bias, (N, F), dtype)
+    for name, t in (("y", y), ("residual", residual), ("pre", pre)):
+        _check_like(name, t, (rows, F), dtype)
+    args = LinearArgs(N, rows, K, F, _dtype_code(x), ACT[act])
+    tensors = dict(x=x, w=w, bias=bias, residual=residual, start=start, y=y, pre=pre)
+    for name, t in tensors.items():
+        setattr(args, name, _ptr(t))
+    args.tensors = tensors
+    return args
+
+
+def smile_linear(args: LinearArgs, stream=None):
+    _check_device(*args.tensors.values())
+    _check(load().smile_linear(C.byref(args), _stream(stream)), "smile_linear")
+
+
+def make_linear_backward_args(dy, x, w, dx=None, dw=None, dbias=None, pre=None, act="none", start=None) -> LinearBackwardArgs:
+    """The argument block of smile_linear_backward; shapes as in make_linear_args.  x and w give the shapes and are always passed."""
+    N, rows, K, F = _linear_shapes(x, w, start)
+    dtype = dy.dtype
+    for name, t, shape in (("dy", dy, (rows, F)), ("x", x, (rows, K)), ("pre", pre, (rows, F)), ("dx", dx, (rows, K))):
+        _check_like(name, t, shape, dtype)
+    for name, t, shape in (("w", w, (N, F, K)), ("dw", dw, (N, F, K)), ("dbias", dbias, (N, F))):
+        _like_grouped(name, t, shape, dtype)
+    args = LinearBackwardArgs(N, rows, K, F, _dtype_code(dy), ACT[act])
+    tensors = dict(dy=dy, x=x, w=w, pre=pre, start=start, dx=dx, dw=dw, dbias=dbias)
+    for name, t in tensors.items():
+        setattr(args, name, _ptr(t))
+    args.tensors = tensors
+    return args
+
+
+def smile_linear_backward_workspace_bytes(args: LinearBackwardArgs) -> int:
+    out = C.c_size_t(0)
+    _check(load().smile_linear_backward_workspace_bytes(C.byref(args), C.byref(out)), "smile_linear_backward_workspace_bytes")
+    return int(out.value)
+
+
+def smile_linear_backward(args: LinearBackwardArgs, workspace=None, stream=None):
+    _check_device(*args.tensors.values(), workspace)
+    _check(load().smile_linear_backward(C.byref(args), _ptr(workspace), _nbytes(workspace), _stream(stream)), "smile_linear_backward")
+
+
+class AdamW:
+    """The tensors of an optimizer step and its plan on their device.  tensors: dicts of param, grad, m, v, and master, m_scale, v_scale or None, all flat or of
+    one shape, with weight_decay; they share their types.  States in uint8 (with scales) make an 8-bit optimizer, in float32 a 32-bit one; zeros are new states."""
+
+    def __init__(self, tensors, beta1=0.9, beta2=0.999, eps=1e-8, seed=0):
+        import torch
+        first = tensors[0]
+        eight = first["m"].dtype == torch.uint8
+        state = torch.uint8 if eight else torch.float32
+        self.tensors = [dict(t) for t in tensors]          # kept alive
+        block = (AdamWTensor * len(tensors))()
+        device = first["param"].device
+        for i, t in enumerate(self.tensors):
+            n = t["param"].numel()
+            padded = -(-n // 128) * 128
+            sizes = dict(param=n, grad=n, master=n, m=padded if eight else n, v=padded if eight else n, m_scale=padded // 128, v_scale=padded // 128)
+            types = dict(param=first["param"].dtype, grad=first["grad"].dtype, master=torch.float32, m=state, v=state, m_scale=torch.uint8, v_scale=torch.uint8)
+            for name, size in sizes.items():
+                x = t.get(name)
+                if (x is None) != (first.get(name) is None):
+                    raise ValueError(f"{name} is given for some tensors only")
+                if x is None:
+                    continue
+                if x.dtype != types[name]:
+                    raise TypeError(f"{name} of tensor {i} is {x.dtype}, not {types[name]}")
+                if x.device != device:
+                    raise ValueError(f"{name} of tensor {i} is on {x.device}, not {device}")
+                if x.numel() != size and not (name.endswith("_scale") and x.numel() >= size):
+                    raise ValueError(f"{name} of tensor {i} has {x.numel()} elements, not {size}")
+                setattr(block[i], name, _ptr(x))
+            block[i].n, block[i].weight_decay = n, float(t.get("weight_decay", 0.0))
+        self.args = AdamWArgs(len(tensors), _dtype_code(first["param"]), _dtype_code(first["grad"]), 8 if eight else 32,
+                              int(first.get("master") is not None), int(seed), float(beta1), float(beta2), float(eps), 0)
+        out = C.c_size_t(0)
+        _check(load().smile_adamw_plan_bytes(C.byref(self.args), block, C.byref(out)), "smile_adamw_plan_bytes")
+        host = torch.empty(out.value + 256, dtype=torch.uint8)
+        at = -host.data_ptr() % 256
+        host = host[at:at + out.value]
+        _check(load().smile_adamw_plan(C.byref(self.args), block, host.data_ptr(), out.value), "smile_adamw_plan")
+        self.plan = host.to(device)
+
+
+def smile_adamw(opt: AdamW, lr, step, stream=None):
+    """One step in place; lr[1] float32 and step[1] int32 on the device.  step is the number of steps made, and goes up by one."""
+    _check_like("lr", lr, (1,), _f32())
+    _check_like("step", step, (1,), _i32())
+    _check_device(opt.plan, lr, step)
+    _check(load().smile_adamw(C.byref(opt.args), opt.plan.data_ptr(), _nbytes(opt.plan), _ptr(lr), _ptr(step), _stream(stream)), "smile_adamw")
+
+
+def smile_adamw_unpack_states(m, m_scale, v, v_scale, m_value, v_value, stream=None):
+    """8-bit states (flat, of whole blocks) as values: float32 or bfloat16."""
+    import torch
+    n = m.numel()
+    for name, t, size in (("m", m, n), ("v", v, n), ("m_value", m_value, n), ("v_value", v_value, n)):
+        if t.numel() != size:
+            raise ValueError(f"{name} has {t.numel()} elements, not {size}")
+    for name, t in (("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale)):
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{name} is {t.dtype}, not {torch.uint8}")
+    for name, t in (("m_scale", m_scale), ("v_scale", v_scale)):
+        if t.numel() * 128 < n:
+            raise ValueError(f"{name} has {t.numel()} elements, of {-(-n // 128)} blocks")
+    if v_value.dtype != m_value.dtype:
+        raise TypeError(f"v_value is {v_value.dtype}, not {m_value.dtype}")
+    _check_device(m, m_scale, v, v_scale, m_value, v_value)
+    _check(load().smile_adamw_unpack_states(n, _dtype_code(m_value), _ptr(m), _ptr(m_scale), _ptr(v), _ptr(v_scale), _ptr(m_value), _ptr(v_value),
+                                            _stream(stream)), "smile_adamw_unpack_states")
 
 
 # ------------------------------------------------------------------ device buffers for one layer

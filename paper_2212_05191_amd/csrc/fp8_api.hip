@@ -1,6 +1,5 @@
 // C-ABI entry points of the 8-bit operators: argument checks, all of them on the host before anything is enqueued.
 #include <algorithm>
-#include <atomic>
 #include <climits>
 #include <cmath>
 
@@ -32,29 +31,6 @@ smile_status check_norm(int T, int d, int dtype)
 {
     const smile_status st = check_rows(1, T, d, dtype);
     return st != SMILE_OK ? st : d > kWidestNorm ? SMILE_BAD_SHAPE : SMILE_OK;
-}
-
-// The compute units of the current device, asked for once per device
-Tuning device_tuning()
-{
-    constexpr int kDevices = 64;
-    static std::atomic<int> known_cus[kDevices];
-    Tuning t;
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) {
-        (void)hipGetLastError();
-        return t;
-    }
-    int cus = known_cus[dev].load(std::memory_order_relaxed);
-    if (cus == 0) {
-        if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
-            (void)hipGetLastError();
-            return t;
-        }
-        known_cus[dev].store(cus, std::memory_order_relaxed);
-    }
-    t.cus = cus;
-    return t;
 }
 
 size_t weight_grad_workspace(int N, int C, int K, int dtype) { return align_up((size_t)N * C * K * elem_size(dtype), 256); }

@@ -1,0 +1,206 @@
+// Products of sorted or dense rows with bias, activation and residual, and their gradients: the choice of kernels, and the kernels beside the products.
+#include "linear_f32.hpp"
+#include "sorted_internal.hpp"
+
+#include <algorithm>
+
+namespace smile {
+
+namespace {
+
+constexpr int kCus = 256;            // what the split of the weights' gradient goes by (its workspace is asked for on the host alone)
+constexpr int kGradRows = 128;       // rows of a part of the bias gradient's sums
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// ---- g = dy act'(pre) in the storage type, and its sums over the rows of each part, before that rounding.  Parts: rows cut at the multiples of
+// kGradRows and at the groups' ends, numbered as in GradWalk.  A workgroup takes 256 columns of a part, 8 a thread, a row in eight.  Bound: HBM (dy and pre
+// read, g written).
+struct GradRows {
+    const void *dy, *pre;
+    const int32_t *start;
+    void *g;                   // or null
+    float *sums;               // [parts][F] or null
+    int N, rows, F, act;
+};
+
+template <typename E>
+__global__ __launch_bounds__(256) void linear_grad_rows_kernel(GradRows a)
+{
+    __shared__ float part[8][256 + 4];
+    int e = 0, above = a.N;
+    const int id = blockIdx.x;
+    while (above - e > 1) {
+        const int mid = (e + above) / 2;
+        if (min(max(a.start[mid], 0), a.rows) / kGradRows + mid <= id) e = mid;
+        else above = mid;
+    }
+    int lo, hi;
+    group_rows(a.start, a.rows, e, lo, hi);
+    const long long begin = (long long)(id - e) * kGradRows;
+    lo = (int)max((long long)lo, begin), hi = (int)min((long long)hi, begin + kGradRows);
+    if (lo >= hi) return;
+    const int col = blockIdx.y * 256 + (threadIdx.x & 31) * 8, sub = threadIdx.x >> 5;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (col < a.F)
+#pragma unroll 4
+        for (int r = lo + sub; r < hi; r += 8) {
+            const size_t at = (size_t)r * a.F + col;
+            Eight<E> d, p;
+            d.load(static_cast<const E *>(a.dy) + at);
+            if (a.act) {
+                p.load(static_cast<const E *>(a.pre) + at);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d.v[i] *= linear_act_grad<sizeof(E) == 4>(a.act, p.v[i]);
+                if (a.g) d.store(static_cast<E *>(a.g) + at);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += d.v[i];
+        }
+    if (!a.sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[sub][(threadIdx.x & 31) * 8 + i] = sum[i];
+    __syncthreads();
+    const int c = blockIdx.y * 256 + threadIdx.x;
+    if (c >= a.F) return;
+    float s = part[0][threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x];
+    a.sums[(size_t)id * a.F + c] = s;
+}
+
+// dbias[e][c] = sum of the parts of group e, in 64 bits and in their order (four threads a column, then theirs)
+template <typename E>
+__global__ __launch_bounds__(256) void linear_bias_sum_kernel(const float *sums, const int32_t *start, E *dbias, int rows, int F)
+{
+    __shared__ double part[4][64];
+    const int e = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 63), sub = threadIdx.x >> 6;
+    int lo, hi;
+    group_rows(start, rows, e, lo, hi);
+    double s = 0.0;
+    if (lo < hi && c < F) {
+        const int first = lo / kGradRows, last = (hi - 1) / kGradRows;
+#pragma unroll 8
+        for (int b = first + sub; b <= last; b += 4) s += (double)sums[(size_t)(b + e) * F + c];
+    }
+    part[sub][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (sub == 0 && c < F) dbias[(size_t)e * F + c] = (E)(float)((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
+}
+
+// dw[e] = sum of the parts of group e, in fp32 in their order.  Bound: HBM (the parts are read once).
+template <typename E>
+__global__ __launch_bounds__(256) void linear_part_sum_kernel(const float *partial, const int32_t *start, E *dw, int rows, int chunk, long long size)
+{
+    const int e = blockIdx.y;
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= size) return;
+    int lo, hi;
+    group_rows(start, rows, e, lo, hi);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (lo < hi)
+#pragma unroll 4
+        for (int b = lo / chunk; b <= (hi - 1) / chunk; ++b) s += *reinterpret_cast<const f32x4 *>(partial + (size_t)(b + e) * size + at);
+    store4(dw + (size_t)e * size + at, s);
+}
+
+// How the sums of the weights' gradient are cut: not at all where the groups' tiles fill the chip, else into parts that do
+struct GradPlan {
+    int chunk, parts;   // 0: whole groups
+    size_t g_at, sums_at, partial_at, total;
+};
+GradPlan grad_plan(const smile_linear_backward_args &a)
+{
+    GradPlan p{};
+    p.parts = a.N;
+    const int tile = kF32Tile;
+    const long long tiles = (long long)a.N * ((a.F + tile - 1) / tile) * ((a.K + tile - 1) / tile), want = 2 * kCus;
+    if (a.dw && tiles < want && a.rows > 256) {
+        const long long cuts = (want + tiles - 1) / tiles * a.N;   // parts of all groups, if they are alike
+        p.chunk = (int)std::max(256ll, (a.rows / cuts + 63) / 64 * 64);
+        p.parts = (a.rows + p.chunk - 1) / p.chunk + a.N - 1;
+    }
+    const bool own_g = a.act != SMILE_ACT_NONE && (a.dx || a.dw);
+    p.sums_at = round256(own_g ? (size_t)a.rows * a.F * elem_size(a.dtype) : 0);
+    p.partial_at = p.sums_at + round256(a.dbias ? ((size_t)(a.rows + kGradRows - 1) / kGradRows + a.N - 1) * a.F * sizeof(float) : 0);
+    p.total = p.partial_at + round256(p.chunk ? (size_t)p.parts * a.F * a.K * sizeof(float) : 0);
+    return p;
+}
+
+int act_of(int act) { return act == SMILE_ACT_NONE ? 0 : act == SMILE_ACT_RELU ? 1 : 2; }
+
+template <typename E, bool GRAD, bool WT>
+hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
+{
+    g.col_tiles = (g.Nout + kF32Tile - 1) / kF32Tile, g.row_tiles = (g.Mrows + kF32Tile - 1) / kF32Tile;
+    const long long most = (GRAD ? (long long)g.parts * g.row_tiles : (g.rows + kF32Tile - 1) / kF32Tile + (long long)g.N - 1) * g.col_tiles;
+    if (most >= 1ll << 31) return hipErrorInvalidValue;
+    const int grid = (int)std::min((most + 7) / 8 * 8, (long long)workgroup_slots(tune, 4));
+    SMILE_LAUNCH((linear_f32_kernel<E, GRAD, WT>), dim3(grid), dim3(256), 0, s, g);
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t forward(const smile_linear_args &a, const Tuning &tune, hipStream_t s)
+{
+    LinearGemm g{};
+    g.x = a.x, g.w = a.w, g.bias = a.bias, g.residual = a.residual, g.y = a.y, g.pre = a.pre, g.start = a.start;
+    g.N = a.N, g.rows = a.rows, g.Nout = a.F, g.K = a.K, g.ldx = a.K, g.ldw = a.K, g.sw = (long long)a.F * a.K, g.act = act_of(a.act);
+    return launch_f32<E, false, false>(g, tune, s);
+}
+
+template <typename E>
+hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, void *workspace, hipStream_t s)
+{
+    const GradPlan p = grad_plan(a);
+    char *ws = static_cast<char *>(workspace);
+    const int act = act_of(a.act);
+    const void *g = a.dy;
+    if ((act && (a.dx || a.dw)) || a.dbias) {
+        GradRows r{a.dy, a.pre, a.start, nullptr, a.dbias ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr, a.N, a.rows, a.F, act};
+        if (act && (a.dx || a.dw)) g = r.g = ws;
+        const int parts = (a.rows + kGradRows - 1) / kGradRows + a.N - 1;
+        SMILE_LAUNCH(linear_grad_rows_kernel<E>, dim3(parts, (a.F + 255) / 256), dim3(256), 0, s, r);
+        if (a.dbias)
+            SMILE_LAUNCH(linear_bias_sum_kernel<E>, dim3((a.F + 63) / 64, a.N), dim3(256), 0, s, (const float *)r.sums, a.start, static_cast<E *>(a.dbias), a.rows, a.F);
+    }
+    if (a.dx) {
+        LinearGemm m{};
+        m.x = g, m.w = a.w, m.y = a.dx, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Nout = a.K, m.K = a.F, m.ldx = a.F, m.ldw = a.K;
+        m.sw = (long long)a.F * a.K;
+        const hipError_t err = launch_f32<E, false, true>(m, tune, s);
+        if (err != hipSuccess) return err;
+    }
+    if (a.dw) {
+        LinearGemm m{};
+        m.x = g, m.w = a.x, m.y = a.dw, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Mrows = a.F, m.Nout = a.K, m.ldx = a.F, m.ldw = a.K;
+        m.sy = (long long)a.F * a.K, m.chunk = p.chunk, m.parts = p.parts;
+        if (p.chunk) m.partial = reinterpret_cast<float *>(ws + p.partial_at);
+        const hipError_t err = launch_f32<E, true, true>(m, tune, s);
+        if (err != hipSuccess) return err;
+        if (p.chunk)
+            SMILE_LAUNCH(linear_part_sum_kernel<E>, dim3((unsigned)((m.sy + 1023) / 1024), a.N), dim3(256), 0, s, (const float *)m.partial, a.start, static_cast<E *>(a.dw),
+                         a.rows, p.chunk, m.sy);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t linear_backward_workspace(const smile_linear_backward_args &a) { return grad_plan(a).total; }
+
+hipError_t launch_linear(const smile_linear_args &a, const Tuning &tune, hipStream_t s)
+{
+    if (a.dtype == SMILE_DTYPE_F32) return forward<float>(a, tune, s);
+    return a.dtype == SMILE_DTYPE_BF16 ? forward<__bf16>(a, tune, s) : forward<_Float16>(a, tune, s);
+}
+
+hipError_t launch_linear_backward(const smile_linear_backward_args &a, const Tuning &tune, void *workspace, hipStream_t s)
+{
+    if (a.dtype == SMILE_DTYPE_F32) return backward<float>(a, tune, workspace, s);
+    return a.dtype == SMILE_DTYPE_BF16 ? backward<__bf16>(a, tune, workspace, s) : backward<_Float16>(a, tune, workspace, s);
+}
+
+}  // namespace smile

@@ -1,0 +1,333 @@
+// k experts for a token: softmax over N columns, the k largest values, their weights, the column sums of the probabilities; and the
+// gradient of the logits.
+//
+// A token is L lanes of a wave, each with V of its values in registers (column 4 (i L + lane) + q, 16 bytes at a time), so that a row is
+// read once and nothing of it is kept anywhere else.  A choice takes the maximum over the lane's values (two a v_max3), over the lanes by
+// DPP, the first column that holds it, and removes that one.  Bound: HBM for many tokens (4 N bytes read each, and 4 N written by
+// the gradient); by instructions where k is large (4.5 V a choice); by latency for few tokens.
+#include "gemm_device.hpp"
+#include "sorted_internal.hpp"
+
+#include <algorithm>
+
+namespace smile {
+
+namespace {
+
+constexpr int kThreads = 256, kMaxBlocks = 512;
+// tokens that one workgroup takes alone, without a second launch for p_sum: lanes of work
+constexpr int kAloneLanes = 4 * kThreads;
+
+// Reductions over the L lanes of a token (L = 4 .. 64, aligned); every lane ends with the same bits
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+template <int L, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, F f)
+{
+    auto step = [&](int other) { v = f(v, __builtin_bit_cast(T, other)); };
+    step(dpp<0xB1>(__builtin_bit_cast(int, v)));                        // quads: 1 0 3 2
+    step(dpp<0x4E>(__builtin_bit_cast(int, v)));                        // 2 3 0 1
+    if constexpr (L >= 8) step(dpp<0x141>(__builtin_bit_cast(int, v)));   // mirrored in 8
+    if constexpr (L >= 16) step(dpp<0x140>(__builtin_bit_cast(int, v)));  // mirrored in 16
+    if constexpr (L >= 32) step(__shfl_xor(__builtin_bit_cast(int, v), 16, 64));
+    if constexpr (L >= 64) step(__shfl_xor(__builtin_bit_cast(int, v), 32, 64));
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float max_over(float v) { return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int L>
+__device__ __forceinline__ int min_over(int v) { return over_lanes<L>(v, [](int a, int b) { return min(a, b); }); }
+template <int L>
+__device__ __forceinline__ float sum_over(float v) { return over_lanes<L>(v, [](float a, float b) { return a + b; }); }
+
+// exp(x), x <= 0, to 2 units of the last place: the exponent's rounding error is multiplied in
+__device__ __forceinline__ float exp_near(float x)
+{
+    const float hi = x * 1.44269504f;
+    const float lo = fmaf(x, 1.44269504f, -hi) + x * 1.92596303e-8f;    // log2(e) = 1.44269504 + 1.926e-8
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return x < -150.f ? 0.f : fmaf(e, lo * 0.69314718f, e);             // (also -infinity, whose lo is NaN)
+}
+
+// The values of token t in this lane, -infinity where there is none
+template <int L, int V>
+__device__ __forceinline__ void load_values(float (&v)[V], const float *logits, const float *bias, int t, int N, int lane)
+{
+    const float *row = logits + (size_t)t * N;
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        const int col = 4 * (i * L + lane);
+        if (!(N & 3)) {
+            f32x4 a = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (col < N) {
+                a = *reinterpret_cast<const f32x4 *>(row + col);
+                if (bias) {
+                    const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + col);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) a[q] = b[q] == -INFINITY ? -INFINITY : a[q] + b[q];
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[4 * i + q] = a[q];
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float a = -INFINITY;
+                if (col + q < N) {
+                    a = row[col + q];
+                    if (bias) a = bias[col + q] == -INFINITY ? -INFINITY : a + bias[col + q];
+                }
+                v[4 * i + q] = a;
+            }
+        }
+    }
+}
+
+// v -> e = exp(v - top); returns 1 / sum (0 for a token without an expert)
+template <int L, int V>
+__device__ __forceinline__ float exponentials(const float (&v)[V], float (&e)[V])
+{
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) top = fmaxf(top, v[i]);
+    top = max_over<L>(top);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = exp_near(v[i] - base), sum += e[i];
+    sum = sum_over<L>(sum);
+    return sum == 0.f ? 0.f : 1.f / sum;
+}
+
+template <int L, int V>
+__global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 3 : 1) void topk_kernel(TopkIo io, int per_block)
+{
+    constexpr int TPB = kThreads / L, MOST = L * V < 64 ? L * V : 64, KR = (MOST + L - 1) / L;
+    const int lane = threadIdx.x % L, slot = threadIdx.x / L;
+    const int first = blockIdx.x * per_block, last = min(io.T, first + per_block);
+    float total[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) total[i] = 0.f;
+    for (int t0 = first; t0 < last; t0 += TPB) {
+        const int t = t0 + slot;
+        const bool live = t < last;
+        float v[V], e[V];
+        load_values<L, V>(v, io.logits, io.bias, min(t, last - 1), io.N, lane);
+        const float inv = exponentials<L, V>(v, e);
+        if (io.partial || io.p_sum) {
+            const float scale = live ? inv : 0.f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) total[i] = live ? fmaf(e[i], scale, total[i]) : total[i];
+        }
+        // the choices: lane j % L keeps the j-th
+        int chosen[KR];
+        float mine[KR], sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < KR; ++r) {
+            chosen[r] = -1, mine[r] = 0.f;
+            for (int jj = 0; jj < L; ++jj) {
+                if (r * L + jj >= io.k) break;
+                float best = v[0];
+#pragma unroll
+                for (int i = 1; i < V; ++i) best = fmaxf(best, v[i]);
+                best = max_over<L>(best);
+                int col = 1 << 30;
+                float ex = 0.f;
+#pragma unroll
+                for (int i = V - 1; i >= 0; --i)
+                    if (v[i] == best) col = 4 * (i / 4) * L + i % 4, ex = e[i];
+                const int at = min_over<L>(col == 1 << 30 ? col : col + 4 * lane);
+                if (best == -INFINITY || at == 1 << 30) break;          // (the second: nothing but NaN is left)
+                const int rel = at - 4 * lane;                          // the lane's value that goes
+                const bool here = col == rel;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (4 * (i / 4) * L + i % 4 == rel) v[i] = -INFINITY;
+                ex = sum_over<L>(here ? ex : 0.f);                      // one lane's value
+                sum += ex;
+                if (lane == jj) chosen[r] = at, mine[r] = ex;
+            }
+        }
+        if (live) {
+            const float scale = !io.normalize || inv != inv ? inv : sum == 0.f ? 0.f : 1.f / sum;   // (NaN stays)
+#pragma unroll
+            for (int r = 0; r < KR; ++r) {
+                const int j = r * L + lane;
+                if (j < io.k) {
+                    io.idx[(size_t)t * io.k + j] = chosen[r];
+                    io.weight[(size_t)t * io.k + j] = chosen[r] < 0 && inv == inv ? 0.f : mine[r] * scale;
+                }
+            }
+        }
+    }
+    if (!io.partial && !io.p_sum) return;
+    // columns of this workgroup: over the tokens of a wave, then of the four waves in their order
+    __shared__ float wave_sum[kThreads / 64][L * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        float s = total[i];
+#pragma unroll
+        for (int off = L; off < 64; off <<= 1) s += __shfl_xor(s, off, 64);
+        if ((threadIdx.x & 63) < L) wave_sum[threadIdx.x >> 6][4 * ((i / 4) * L + lane) + i % 4] = s;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < io.N; c += kThreads) {
+        const float s = (wave_sum[0][c] + wave_sum[1][c]) + (wave_sum[2][c] + wave_sum[3][c]);
+        if (io.partial) io.partial[(size_t)blockIdx.x * io.N + c] = s;
+        else io.p_sum[c] = s;
+    }
+}
+
+// p_sum[c] = sum over the workgroups' rows of partial[blocks][N], in 64 bits: four columns a workgroup, 64 threads each
+__global__ __launch_bounds__(kThreads) void topk_sum_kernel(const float *partial, float *p_sum, int blocks, int N)
+{
+    __shared__ double part[kThreads];
+    const int c = blockIdx.x * 4 + threadIdx.x % 4, row0 = threadIdx.x / 4;
+    double s = 0.0;
+    if (c < N)
+#pragma unroll 8
+        for (int b = row0; b < blocks; b += kThreads / 4) s += (double)partial[(size_t)b * N + c];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    for (int n = kThreads / 2; n >= 4; n >>= 1) {
+        if ((int)threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
+        __syncthreads();
+    }
+    if (threadIdx.x < 4 && c < N) p_sum[c] = (float)part[threadIdx.x];
+}
+
+// dlogits = p (u - sum p u), + w (dweight - sum w dweight) at the chosen columns of normalised weights.  The chosen values are gathered through the
+// token's lanes: each lane compares the columns that it holds.
+template <int L, int V>
+__global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 3 : 1) void topk_backward_kernel(TopkGradIo io)
+{
+    const int lane = threadIdx.x % L;
+    const long long id = (long long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    if (id >= io.T) return;
+    const int t = (int)id;
+    float v[V], p[V], u[V];
+    load_values<L, V>(v, io.logits, io.bias, t, io.N, lane);
+    const float inv = exponentials<L, V>(v, p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int col = 4 * ((i / 4) * L + lane) + i % 4;
+        p[i] *= inv;
+        u[i] = 0.f;
+        if (io.count && col < io.N) u[i] = io.coef * (float)io.count[col];
+        v[i] = 0.f;                                                     // from here on: the gradient that reaches a chosen column
+    }
+    const size_t at = (size_t)t * io.k;
+    std::conditional_t<(V > 32), uint64_t, uint32_t> picked = 0;        // of the lane's values
+    constexpr decltype(picked) one = 1;
+#pragma unroll 1
+    for (int j = 0; j < io.k; ++j) {
+        const int col = io.idx[at + j], rel = col < io.N ? col - 4 * lane : -1;
+        const float dw = io.dweight[at + j];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += 4 * (i / 4) * L + i % 4 == rel ? dw : 0.f;
+        if (rel >= 0 && rel % (4 * L) < 4) picked |= one << (rel / (4 * L) * 4 + rel % 4);
+    }
+    float of_chosen = 0.f, sum = 0.f, dot = 0.f;
+    if (io.normalize) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (picked >> i & 1) sum += p[i], dot = fmaf(p[i], v[i], dot);
+        sum = sum_over<L>(sum), dot = sum_over<L>(dot);
+        of_chosen = sum == 0.f ? 0.f : 1.f / sum;
+        dot *= of_chosen;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (picked >> i & 1) u[i] += v[i];
+    }
+    float mean = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) mean = fmaf(p[i], u[i], mean);
+    mean = sum_over<L>(mean);
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        const int col = 4 * (i * L + lane);
+        f32x4 d;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = 4 * i + q;
+            d[q] = p[n] * (u[n] - mean);
+            if (io.normalize && (picked >> n & 1)) d[q] = fmaf(p[n] * of_chosen, v[n] - dot, d[q]);
+        }
+        float *to = io.dlogits + (size_t)t * io.N + col;
+        if (!(io.N & 3)) {
+            if (col < io.N) *reinterpret_cast<f32x4 *>(to) = d;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (col + q < io.N) to[q] = d[q];
+        }
+    }
+}
+
+// f(lanes, values) of the smallest shape that holds N columns
+template <typename F>
+auto with_shape(int N, F &&f)
+{
+#define SMILE_SHAPE(l, v) return f(std::integral_constant<int, l>{}, std::integral_constant<int, v>{})
+    if (N <= 16) SMILE_SHAPE(4, 4);
+    if (N <= 32) SMILE_SHAPE(4, 8);
+    if (N <= 64) SMILE_SHAPE(8, 8);
+    if (N <= 128) SMILE_SHAPE(8, 16);
+    if (N <= 256) SMILE_SHAPE(16, 16);
+    if (N <= 512) SMILE_SHAPE(32, 16);
+    if (N <= 1024) SMILE_SHAPE(64, 16);
+    if (N <= 2048) SMILE_SHAPE(64, 32);
+    SMILE_SHAPE(64, 64);
+#undef SMILE_SHAPE
+}
+
+int lanes(int N) { return with_shape(N, [](auto l, auto) { return (int)decltype(l)::value; }); }
+
+// tokens of a workgroup (a whole number of rounds of its lanes) and workgroups
+void plan(int T, int N, int &per_block, int &blocks)
+{
+    const int tpb = kThreads / lanes(N);
+    if ((long long)T * lanes(N) <= kAloneLanes) {
+        per_block = T, blocks = 1;
+        return;
+    }
+    const int rounds = (T + tpb - 1) / tpb;
+    per_block = (rounds + kMaxBlocks - 1) / kMaxBlocks * tpb;
+    blocks = (T + per_block - 1) / per_block;
+}
+
+}  // namespace
+
+size_t topk_workspace(int T, int N)
+{
+    int per_block, blocks;
+    plan(T, N, per_block, blocks);
+    return blocks > 1 ? (size_t)blocks * N * sizeof(float) : 0;
+}
+
+hipError_t launch_topk(const TopkIo &given, hipStream_t s)
+{
+    TopkIo io = given;
+    int per_block, blocks;
+    plan(io.T, io.N, per_block, blocks);
+    if (!io.p_sum || blocks == 1) io.partial = nullptr;
+    with_shape(io.N, [&](auto l, auto v) {
+        SMILE_LAUNCH((topk_kernel<decltype(l)::value, decltype(v)::value>), dim3(blocks), dim3(kThreads), 0, s, io, per_block);
+        return 0;
+    });
+    if (io.partial) SMILE_LAUNCH(topk_sum_kernel, dim3((io.N + 3) / 4), dim3(kThreads), 0, s, (const float *)io.partial, io.p_sum, blocks, io.N);
+    return hipGetLastError();
+}
+
+hipError_t launch_topk_backward(const TopkGradIo &io, hipStream_t s)
+{
+    with_shape(io.N, [&](auto l, auto v) {
+        const int tpb = kThreads / decltype(l)::value;
+        SMILE_LAUNCH((topk_backward_kernel<decltype(l)::value, decltype(v)::value>), dim3((io.T + tpb - 1) / tpb), dim3(kThreads), 0, s, io);
+        return 0;
+    });
+    return hipGetLastError();
+}
+
+}  // namespace smile

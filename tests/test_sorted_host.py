@@ -1,0 +1,212 @@
+"""Host side of the operators of a layer without dropped tokens and of its optimizer: argument checks (which run before anything touches a GPU), sizes, the
+binding's checks, the plan of an optimizer step, and the reference itself against differences.  No kernel is launched here."""
+import ctypes as C
+
+import pytest
+import torch
+
+import sorted_reference as R
+from paper_2212_05191_amd import binding as B
+
+P = 4096          # a pointer that is aligned and never followed
+ODD = P + 4       # one that is not
+BIG = 1 << 40
+
+
+def test_topk_refusals():
+    lib = B.load()
+
+    def call(T=4, N=8, k=2, logits=P, bias=P, idx=P, weight=P, p_sum=P, workspace=P, nbytes=BIG):
+        return lib.smile_topk(T, N, k, 1, logits, bias, idx, weight, p_sum, workspace, nbytes, None)
+
+    for name in ("logits", "idx", "weight"):
+        assert call(**{name: None}) == B.INVALID_ARG, name
+    for name in ("logits", "bias", "idx", "weight", "p_sum"):
+        assert call(**{name: ODD}) == B.INVALID_ARG, name
+    for bad in (dict(T=0), dict(N=0), dict(N=4097), dict(k=0), dict(k=9), dict(k=65, N=100), dict(T=1 << 25), dict(T=-1)):
+        assert call(**bad) == B.BAD_SHAPE, bad
+    assert call(T=100000, workspace=None) == B.INVALID_ARG and call(T=100000, workspace=P + 16) == B.WORKSPACE
+    assert call(T=100000, nbytes=B.smile_topk_workspace_bytes(100000, 8) - 1) == B.WORKSPACE
+
+    def back(T=4, N=8, k=2, logits=P, bias=P, idx=P, dweight=P, count=P, dlogits=P):
+        return lib.smile_topk_backward(T, N, k, 0, logits, bias, idx, dweight, count, 1.0, dlogits, None)
+
+    for name in ("logits", "idx", "dweight", "dlogits"):
+        assert back(**{name: None}) == B.INVALID_ARG, name
+    for name in ("logits", "bias", "idx", "dweight", "count", "dlogits"):
+        assert back(**{name: ODD}) == B.INVALID_ARG, name
+    assert back(T=0) == B.BAD_SHAPE and back(k=9) == B.BAD_SHAPE
+
+
+def test_sort_refusals():
+    lib = B.load()
+
+    def call(T=4, k=2, N=8, idx=P, count=P, start=P, pos=P, source=P, workspace=P, nbytes=BIG):
+        return lib.smile_sort_experts(T, k, N, idx, count, start, pos, source, workspace, nbytes, None)
+
+    for name in ("idx", "count", "start", "pos", "source"):
+        assert call(**{name: None}) == B.INVALID_ARG and call(**{name: ODD}) == B.INVALID_ARG, name
+    for bad in (dict(T=0), dict(k=0), dict(k=65), dict(N=0), dict(N=4097), dict(T=1 << 25, k=2)):
+        assert call(**bad) == B.BAD_SHAPE, bad
+    assert call(T=100000, workspace=None) == B.INVALID_ARG and call(T=100000, workspace=P + 128) == B.WORKSPACE
+    assert call(T=100000, nbytes=B.smile_sort_experts_workspace_bytes(100000, 2, 8) - 1) == B.WORKSPACE
+
+
+def test_row_refusals():
+    lib = B.load()
+
+    def dispatch(T=4, k=2, d=64, R_=8, dtype=1, x=P, pos=P, xs=P):
+        return lib.smile_sorted_dispatch(T, k, d, R_, dtype, x, pos, xs, None)
+
+    def combine(T=4, k=2, d=64, R_=8, dtype=1, ys=P, pos=P, weight=P, residual=P, y=P):
+        return lib.smile_sorted_combine(T, k, d, R_, dtype, ys, pos, weight, residual, y, None)
+
+    def back(T=4, k=2, d=64, R_=8, dtype=1, dy=P, ys=P, pos=P, weight=P, dys=2 * P, dweight=P):
+        return lib.smile_sorted_combine_backward(T, k, d, R_, dtype, dy, ys, pos, weight, dys, dweight, None)
+
+    for f, needed, all_ in ((dispatch, ("x", "pos", "xs"), ("x", "pos", "xs")), (combine, ("ys", "pos", "y"), ("ys", "pos", "weight", "residual", "y")),
+                            (back, ("dy", "pos", "weight", "dys"), ("dy", "ys", "pos", "weight", "dys", "dweight"))):
+        for name in needed:
+            assert f(**{name: None}) == B.INVALID_ARG, (f, name)
+        for name in all_:
+            assert f(**{name: ODD}) == B.INVALID_ARG, (f, name)
+        for bad in (dict(T=0), dict(k=0), dict(k=65), dict(R_=0), dict(R_=(1 << 27) + 1), dict(d=0), dict(d=12), dict(d=16392), dict(T=1 << 26, k=1)):
+            assert f(**bad) == B.BAD_SHAPE, (f, bad)
+        assert f(dtype=3) == B.UNSUPPORTED and f(dtype=-1) == B.UNSUPPORTED
+    assert back(ys=None) == B.INVALID_ARG and back(dweight=None) == B.INVALID_ARG and back(dys=P) == B.INVALID_ARG
+
+
+def test_linear_refusals():
+    lib = B.load()
+
+    def args(cls, **kw):
+        a = cls(*(kw.pop(n, v) for n, v in (("N", 2), ("rows", 16), ("K", 64), ("F", 64), ("dtype", 1), ("act", 1))))
+        for i, (name, _) in enumerate(cls._fields_[6:]):
+            setattr(a, name, kw.pop(name, P * (i + 1)))
+        assert not kw
+        return a
+
+    call = lambda **kw: lib.smile_linear(C.byref(args(B.LinearArgs, **kw)), None)                                                # noqa: E731
+    size = C.c_size_t(0)
+    need = lambda **kw: lib.smile_linear_backward_workspace_bytes(C.byref(args(B.LinearBackwardArgs, **kw)), C.byref(size))      # noqa: E731
+    back = lambda ws=P, n=BIG, **kw: lib.smile_linear_backward(C.byref(args(B.LinearBackwardArgs, **kw)), ws, n, None)           # noqa: E731
+    assert lib.smile_linear(None, None) == B.INVALID_ARG and lib.smile_linear_backward(None, P, BIG, None) == B.INVALID_ARG
+    for name in ("x", "w", "y", "start"):                  # start: N is 2
+        assert call(**{name: None}) == B.INVALID_ARG, name
+    for name in ("x", "w", "bias", "residual", "start", "y", "pre"):
+        assert call(**{name: ODD}) == B.INVALID_ARG, name
+    assert call(y=P) == B.INVALID_ARG and call(pre=6 * P) == B.INVALID_ARG and call(pre=4 * P) == B.INVALID_ARG     # y is x; pre is y, the residual
+    for name in ("dy", "start"):
+        assert back(**{name: None}) == B.INVALID_ARG and need(**{name: None}) == B.INVALID_ARG, name
+    for name in ("dy", "x", "w", "pre", "start", "dx", "dw", "dbias"):
+        assert back(**{name: ODD}) == B.INVALID_ARG and need(**{name: ODD}) == B.INVALID_ARG, name
+    assert back(dx=None, dw=None, dbias=None) == B.INVALID_ARG                             # nothing to compute
+    assert back(w=None) == B.INVALID_ARG and back(x=None) == B.INVALID_ARG and back(pre=None) == B.INVALID_ARG
+    assert need(w=None, dx=None) == B.OK and need(x=None, dw=None) == B.OK and need(pre=None, act=2) == B.OK
+    for f in (call, back, need):
+        for bad in (dict(N=0), dict(N=4097), dict(rows=0), dict(rows=(1 << 27) + 1), dict(K=0), dict(K=12), dict(K=32776), dict(F=0), dict(F=20), dict(F=32776),
+                    dict(rows=1 << 27, K=16384), dict(N=4096, K=32768, F=32768)):
+            assert f(**bad) == B.BAD_SHAPE, bad
+        assert f(dtype=3) == B.UNSUPPORTED and f(dtype=-1) == B.UNSUPPORTED and f(act=3) == B.UNSUPPORTED and f(act=-1) == B.UNSUPPORTED
+    assert need() == B.OK and size.value > 0
+    assert back(ws=None) == B.INVALID_ARG and back(ws=P + 16) == B.WORKSPACE and back(n=size.value - 1) == B.WORKSPACE
+
+
+def adam(n=300, bits=8, master=True, dtype=torch.bfloat16, grad=torch.float32):
+    blocks = -(-n // 128)
+    t = dict(param=torch.zeros(n, dtype=dtype), grad=torch.zeros(n, dtype=grad), master=torch.zeros(n) if master else None)
+    if bits == 8:
+        return {**t, "m": torch.zeros(blocks * 128, dtype=torch.uint8), "v": torch.zeros(blocks * 128, dtype=torch.uint8), "m_scale": torch.zeros(blocks, dtype=torch.uint8),
+                "v_scale": torch.zeros(blocks, dtype=torch.uint8)}
+    return {**t, "m": torch.zeros(n), "v": torch.zeros(n)}
+
+
+def test_adamw_plan_lists_every_chunk():
+    opt = B.AdamW([adam(n) for n in (1, 2048, 2049, 9000)])
+    assert opt.args.chunks == 1 + 1 + 2 + 5 and opt.args.state_bits == 8 and opt.args.has_master == 1
+    words = opt.plan[opt.plan.numel() - 8 * 9:].view(torch.int32).view(-1, 2).tolist()
+    assert words == [[0, 0], [1, 0], [2, 0], [2, 1]] + [[3, c] for c in range(5)]
+    assert bool((opt.plan[:256] == 0).all())
+
+
+def test_adamw_refusals():
+    lib = B.load()
+    for wrong, error in ((dict(grad=torch.zeros(299)), ValueError), (dict(m=torch.zeros(300, dtype=torch.uint8)), ValueError), (dict(v=torch.zeros(384)), TypeError),
+                         (dict(master=torch.zeros(300, dtype=torch.float64)), TypeError), (dict(v_scale=torch.zeros(2, dtype=torch.uint8)), ValueError),
+                         (dict(grad=torch.zeros(300, dtype=torch.float16)), B.SmileError), (dict(param=torch.zeros(300, dtype=torch.int32)), TypeError),
+                         (dict(v_scale=None), B.SmileError), (dict(weight_decay=float("inf")), B.SmileError)):
+        with pytest.raises(error):
+            B.AdamW([{**adam(), **wrong}])
+    with pytest.raises(ValueError):
+        B.AdamW([adam(), adam(master=False)])
+    with pytest.raises(TypeError):
+        B.AdamW([adam(), adam(dtype=torch.float16)])
+    for wrong in (dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0), dict(eps=2.0), dict(beta1=float("nan"))):
+        with pytest.raises(B.SmileError) as e:
+            B.AdamW([adam()], **wrong)
+        assert e.value.status == B.BAD_SHAPE
+    with pytest.raises(B.SmileError) as e:                                  # a master of 32-bit parameters
+        B.AdamW([adam(dtype=torch.float32)])
+    assert e.value.status == B.UNSUPPORTED
+    opt = B.AdamW([adam()])
+    call = lambda plan=P, nbytes=opt.plan.numel(), lr=P, step=P: lib.smile_adamw(C.byref(opt.args), plan, nbytes, lr, step, None)    # noqa: E731
+    assert call(plan=None) == B.INVALID_ARG and call(lr=None) == B.INVALID_ARG and call(step=None) == B.INVALID_ARG
+    assert call(lr=P + 2) == B.INVALID_ARG and call(step=P + 1) == B.INVALID_ARG
+    assert call(plan=P + 16) == B.WORKSPACE and call(nbytes=opt.plan.numel() - 1) == B.WORKSPACE
+    unpack = lambda n=256, dtype=0, m=P, ms=P, v=P, vs=P, mv=P, vv=P: lib.smile_adamw_unpack_states(n, dtype, m, ms, v, vs, mv, vv, None)    # noqa: E731
+    for bad in (dict(m=None), dict(ms=None), dict(v=ODD), dict(vs=None), dict(mv=None), dict(vv=ODD)):
+        assert unpack(**bad) == B.INVALID_ARG, bad
+    assert unpack(n=100) == B.BAD_SHAPE and unpack(n=0) == B.BAD_SHAPE and unpack(dtype=2) == B.UNSUPPORTED
+
+
+def test_binding_refuses_shapes_and_types():
+    f32, i32 = torch.float32, torch.int32
+    z = torch.zeros
+    with pytest.raises(TypeError):
+        B.smile_topk(z(4, 8, dtype=torch.bfloat16), z(4, 2, dtype=i32), z(4, 2))
+    with pytest.raises(ValueError):
+        B.smile_topk(z(4, 8), z(4, 2, dtype=i32), z(4, 3))
+    with pytest.raises(ValueError):
+        B.smile_topk_backward(z(4, 8), z(4, 2, dtype=i32), z(4, 2), z(4, 7))
+    with pytest.raises(ValueError):
+        B.smile_sort_experts(z(4, 2, dtype=i32), z(8, dtype=i32), z(8, dtype=i32), z(4, 2, dtype=i32), z(8, dtype=i32))
+    with pytest.raises(TypeError):
+        B.smile_sorted_dispatch(z(4, 64), z(4, 2, dtype=torch.int64), z(8, 64))
+    with pytest.raises(ValueError):
+        B.smile_sorted_combine(z(8, 64), z(4, 2, dtype=i32), z(4, 72))
+    with pytest.raises(ValueError):
+        B.smile_sorted_combine_backward(z(4, 64), z(7, 64), z(4, 2, dtype=i32), z(4, 2), z(8, 64), z(4, 2))
+    x, w, y = z(4, 64), z(2, 72, 64), z(4, 72)
+    for wrong in (dict(w=z(2, 72, 56)), dict(y=z(4, 64)), dict(bias=z(72)), dict(residual=z(3, 72)), dict(start=z(2, dtype=i32)), dict(pre=z(4, 71))):
+        with pytest.raises(ValueError):
+            B.make_linear_args(**{**dict(x=x, w=w, y=y, start=z(3, dtype=i32)), **wrong})
+    for wrong in (dict(w=w.half()), dict(bias=z(2, 72, dtype=torch.float16)), dict(start=z(3, dtype=torch.int64))):
+        with pytest.raises(TypeError):
+            B.make_linear_args(**{**dict(x=x, w=w, y=y, start=z(3, dtype=i32)), **wrong})
+    with pytest.raises(AssertionError):                     # rows of another stride
+        B.make_linear_args(x=z(4, 128)[:, ::2], w=w, y=y, start=z(3, dtype=i32))
+    with pytest.raises(ValueError):
+        B.make_linear_backward_args(y, x, w, dx=z(4, 72), start=z(3, dtype=i32))
+
+
+def test_reference_gradients_against_differences():
+    g = torch.Generator().manual_seed(1)
+    n = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)        # noqa: E731
+    start = torch.tensor([0, 3, 3, 9])
+    x, w, b, dy, vx, vw, vb = n(9, 5), n(3, 4, 5), n(3, 4), n(9, 4), n(9, 5), n(3, 4, 5), n(3, 4)
+    for name in ("none", "gelu"):
+        def loss(h):
+            return float((R.linear(x + h * vx, w + h * vw, b + h * vb, name, None, start)[0] * dy).sum())
+        out = R.linear_backward(dy, x, w, R.linear(x, w, b, name, None, start)[1], name, start)
+        total = sum(float((out[k][0] * v).sum()) for k, v in (("dx", vx), ("dw", vw), ("dbias", vb)))
+        assert abs((loss(1e-6) - loss(-1e-6)) / 2e-6 - total) < 1e-6 * (1 + abs(total))
+    logits, dweight, count, v = n(6, 7).float(), n(6, 3).float(), torch.arange(7, dtype=torch.int32), n(6, 7)
+    for normalize in (False, True):
+        idx, weight, p, _ = R.topk(logits, None, 3, normalize)
+        grad, _ = R.topk_backward(p, idx, weight, dweight, normalize, count, 0.1)
+
+        def loss(h):
+            p = torch.softmax(logits.double() + h * v, 1)
+            ww = p.gather(1, idx.long())
+            return float((dweight.double() * (ww / ww.sum(1, keepdim=True) if normalize else ww)).sum() + 0.1 * (count.double() * p.sum(0)).sum())
+        assert abs((loss(1e-6) - loss(-1e-6)) / 2e-6 - float((grad * v).sum())) < 1e-6
