@@ -3,12 +3,12 @@
 #include "sorted_internal.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace smile {
 
 namespace {
 
-constexpr int kCus = 256;            // what the split of the weights' gradient goes by (its workspace is asked for on the host alone)
 constexpr int kGradRows = 128;       // rows of a part of the bias gradient's sums
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -115,8 +115,8 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
 {
     GradPlan p{};
     p.parts = a.N;
-    const int tile = kF32Tile;
-    const long long tiles = (long long)a.N * ((a.F + tile - 1) / tile) * ((a.K + tile - 1) / tile), want = 2 * kCus;
+    const int tile = a.dtype == SMILE_DTYPE_F32 ? kF32Tile : pick_half_tile(kLinearWeightGrad, a.N, a.rows, a.F, a.K, 0) == kHalf256 ? 256 : 128;
+    const long long tiles = (long long)a.N * ((a.F + tile - 1) / tile) * ((a.K + tile - 1) / tile), want = tile == 256 ? kLinearCus : 2 * kLinearCus;
     if (a.dw && tiles < want && a.rows > 256) {
         const long long cuts = (want + tiles - 1) / tiles * a.N;   // parts of all groups, if they are alike
         p.chunk = (int)std::max(256ll, (a.rows / cuts + 63) / 64 * 64);
@@ -132,6 +132,9 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
 int act_of(int act) { return act == SMILE_ACT_NONE ? 0 : act == SMILE_ACT_RELU ? 1 : 2; }
 
 template <typename E, bool GRAD, bool WT>
+hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s);
+
+template <typename E, bool GRAD, bool WT>
 hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
 {
     g.col_tiles = (g.Nout + kF32Tile - 1) / kF32Tile, g.row_tiles = (g.Mrows + kF32Tile - 1) / kF32Tile;
@@ -142,13 +145,23 @@ hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
     return hipGetLastError();
 }
 
+template <typename E, bool GRAD, bool WT>
+hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s)
+{
+    if constexpr (sizeof(E) == 4) return launch_f32<E, GRAD, WT>(g, tune, s);
+    else {
+        const LinearKind kind = GRAD ? kLinearWeightGrad : WT ? kLinearRowGrad : kLinearForward;
+        return launch_linear_half(std::is_same_v<E, __bf16> ? SMILE_DTYPE_BF16 : SMILE_DTYPE_F16, g, kind, pick_half_tile(kind, g.N, g.rows, g.Mrows, g.Nout, g.act), tune, s);
+    }
+}
+
 template <typename E>
 hipError_t forward(const smile_linear_args &a, const Tuning &tune, hipStream_t s)
 {
     LinearGemm g{};
     g.x = a.x, g.w = a.w, g.bias = a.bias, g.residual = a.residual, g.y = a.y, g.pre = a.pre, g.start = a.start;
     g.N = a.N, g.rows = a.rows, g.Nout = a.F, g.K = a.K, g.ldx = a.K, g.ldw = a.K, g.sw = (long long)a.F * a.K, g.act = act_of(a.act);
-    return launch_f32<E, false, false>(g, tune, s);
+    return launch_product<E, false, false>(g, tune, s);
 }
 
 template <typename E>
@@ -170,7 +183,7 @@ hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, voi
         LinearGemm m{};
         m.x = g, m.w = a.w, m.y = a.dx, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Nout = a.K, m.K = a.F, m.ldx = a.F, m.ldw = a.K;
         m.sw = (long long)a.F * a.K;
-        const hipError_t err = launch_f32<E, false, true>(m, tune, s);
+        const hipError_t err = launch_product<E, false, true>(m, tune, s);
         if (err != hipSuccess) return err;
     }
     if (a.dw) {
@@ -178,7 +191,7 @@ hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, voi
         m.x = g, m.w = a.x, m.y = a.dw, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Mrows = a.F, m.Nout = a.K, m.ldx = a.F, m.ldw = a.K;
         m.sy = (long long)a.F * a.K, m.chunk = p.chunk, m.parts = p.parts;
         if (p.chunk) m.partial = reinterpret_cast<float *>(ws + p.partial_at);
-        const hipError_t err = launch_f32<E, true, true>(m, tune, s);
+        const hipError_t err = launch_product<E, true, true>(m, tune, s);
         if (err != hipSuccess) return err;
         if (p.chunk)
             SMILE_LAUNCH(linear_part_sum_kernel<E>, dim3((unsigned)((m.sy + 1023) / 1024), a.N), dim3(256), 0, s, (const float *)m.partial, a.start, static_cast<E *>(a.dw),

@@ -1,0 +1,34 @@
+// The products of smile_linear and of its gradients, as their launchers take them.
+#pragma once
+
+#include "smile_internal.hpp"
+
+namespace smile {
+
+// One product, y(i, j) = sum_k X(i, k) W(j, k) per group e.
+//   rows (forward, gradient of x): X is the group's rows of x [rows][ldx], W = w[e] [Nout][K], or [K][Nout] where the kernel takes it transposed
+//   weights' gradient: X(i, r) = x[r][i], W(j, r) = w[r][j], summed over the group's rows r; y[e] is [Mrows][Nout]
+struct LinearGemm {
+    const void *x, *w;
+    const void *bias, *residual;   // [N][Nout], [rows][Nout]
+    void *y, *pre;
+    const int32_t *start;          // [N+1] or null: one group of all rows
+    float *partial;                // weights' gradient whose sums are cut: [parts][Mrows][Nout]
+    int N, rows;
+    int Mrows, Nout, K;
+    int ldx, ldw;                  // elements
+    long long sw, sy;              // elements of a group in w, in y
+    int row_tiles, col_tiles;      // (row_tiles: weights' gradient)
+    int chunk, parts;              // rows of a part of the sum (0: whole groups), and the parts of all groups
+    int act;                       // 0 none, 1 ReLU, 2 GELU
+};
+
+enum LinearKind { kLinearForward, kLinearRowGrad, kLinearWeightGrad };
+// Tiles of the 16-bit kernel: 256 x 256 alone on a CU, 128 x 128 two on a CU
+enum HalfTile { kHalf256, kHalf128 };
+// what the choice of a tile and the split of the weights' gradient go by: the latter's workspace is asked for on the host alone
+constexpr int kLinearCus = 256;
+HalfTile pick_half_tile(LinearKind kind, int N, int rows, int Mrows, int Nout, int act);
+hipError_t launch_linear_half(int dtype, const LinearGemm &g, LinearKind kind, HalfTile tile, const Tuning &tune, hipStream_t s);
+
+}  // namespace smile

@@ -2,26 +2,9 @@
 #pragma once
 
 #include "gemm_device.hpp"
+#include "linear_internal.hpp"
 
 namespace smile {
-
-// One product, y(i, j) = sum_k X(i, k) W(j, k) per group e.
-//   rows (forward, gradient of x): X is the group's rows of x [rows][ldx], W = w[e] [Nout][K], or [K][Nout] where the kernel takes it transposed
-//   weights' gradient: X(i, r) = x[r][i], W(j, r) = w[r][j], summed over the group's rows r; y[e] is [Mrows][Nout]
-struct LinearGemm {
-    const void *x, *w;
-    const void *bias, *residual;   // [N][Nout], [rows][Nout]
-    void *y, *pre;
-    const int32_t *start;          // [N+1] or null: one group of all rows
-    float *partial;                // weights' gradient whose sums are cut: [parts][Mrows][Nout]
-    int N, rows;
-    int Mrows, Nout, K;
-    int ldx, ldw;                  // elements
-    long long sw, sy;              // elements of a group in w, in y
-    int row_tiles, col_tiles;      // (row_tiles: weights' gradient)
-    int chunk, parts;              // rows of a part of the sum (0: whole groups), and the parts of all groups
-    int act;                       // 0 none, 1 ReLU, 2 GELU
-};
 
 namespace {
 
@@ -34,15 +17,18 @@ struct LinearTile {
     int part;
 };
 
-// rows [lo, hi) of group g, whatever `start` holds
+// rows [lo, hi) of group g, whatever `start` holds.  Read through the constant address space: with a uniform g by the scalar unit, whose counter is not that of
+// the loads in flight.
 __device__ __forceinline__ void group_rows(const int32_t *start, int rows, int g, int &lo, int &hi)
 {
     if (!start) {
         lo = 0, hi = rows;
         return;
     }
-    lo = min(max(start[g], 0), rows);
-    hi = min(max(start[g + 1], lo), rows);
+    typedef const __attribute__((address_space(4))) int32_t *constant;
+    const constant s = (constant)(uintptr_t)start;
+    lo = min(max(s[g], 0), rows);
+    hi = min(max(s[g + 1], lo), rows);
 }
 
 // Live row tiles of groups whose first rows the device alone knows.  Lane c of every wave holds the row tiles of groups 64 c .. 64 c + 63 and their
