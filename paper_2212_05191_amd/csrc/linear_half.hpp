@@ -1,13 +1,14 @@
 // Products over sorted rows on the 16-bit matrix instructions (v_mfma_f32_32x32x16): rows (forward, gradient of x) and the weights' gradient.
 //
 // A workgroup of WM x WN waves computes BM x BN outputs at a time, a wave (64 QA) x 64 of them, and walks the tiles of the launch.  A slab (64 terms) is four
-// units: the rows of X of the first and of the second half of every wave's blocks (A0, A1), and the same of W (B0, B1).  The four products of a slab are its
-// phases, in the order A0 B0, A0 B1, A1 B1, A1 B0: a phase reads what it does not hold yet from LDS and multiplies.  LDS holds two slabs; a unit's slot is refilled
-// one phase after its reading, two slabs ahead, so that five to seven of the eight units are in flight at any time.  The stream of slabs runs on through the
+// units: the rows of X of the first and of the second half of every wave's blocks (A0, A1), and the same of W (B0, B1).  It is multiplied in two phases: A0 with B0
+// and B1, then A1; a phase reads what it does not hold yet from LDS and multiplies.  LDS holds two slabs; a unit's slot is refilled
+// one phase after its reading, two slabs ahead, so that four to five of the eight units are in flight at any time (with four phases of one product five to seven are, but
+// twice the barriers cost more: 8192^3 1017 -> 971 us).  The stream of slabs runs on through the
 // tiles: the epilogue finds the next tile's first two slabs requested.  Behind the last tile the last slab is requested again, so that every wait
 // counts the same.
 //
-// What bounds it: the matrix cores, if what they are fed with keeps up.  A wave that reads its fragments (up to 12 of 16 bytes a lane) cannot multiply, so two waves
+// What bounds it: the matrix cores, if what they are fed with keeps up.  A wave that reads its fragments (up to 16 of 16 bytes a lane) cannot multiply, so two waves
 // of a SIMD take turns (STAGGER): the waves are two halves, one a barrier behind the other; while one multiplies the other reads and requests.  With
 // four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.
 //
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
     constexpr int kOff[4] = {0, UA * 128, (UA + UB) * 128, (UA + 2 * UB) * 128};
     constexpr int STAGE = 2 * (UA + UB) * 128;
     static_assert(UA == UB && UA / (8 * NW) == 2, "two load instructions a wave and unit");
-    constexpr int kAhead = 10;   // load instructions behind the unit that the next phase reads: five units
+    constexpr int kAhead = 8;    // load instructions behind the units that the next phase reads: four units
     __shared__ __attribute__((aligned(16))) char half_lds_[half_lds<WM, WN, QA>()];
     lds_char *const lds = (lds_char *)half_lds_;
 
@@ -202,37 +203,36 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
         constexpr int P = decltype(number)::value;
         // the stage read and the stage filled do not overlap
         auto fetch = [&](const lds_char *__restrict stage) __attribute__((always_inline)) {
-            if constexpr (P == 0) read_unit(std::integral_constant<int, A0>{}, stage), read_unit(std::integral_constant<int, B0>{}, stage);
-            if constexpr (P == 1) read_unit(std::integral_constant<int, B1>{}, stage);
-            if constexpr (P == 2) {
-                if (upper) read_unit(std::integral_constant<int, A1>{}, stage);
-            }
             if constexpr (P == 0) {
+                read_unit(std::integral_constant<int, A0>{}, stage);
+                read_unit(std::integral_constant<int, B0>{}, stage), read_unit(std::integral_constant<int, B1>{}, stage);
                 if (fresh != 0) load_unit(std::integral_constant<int, A1>{});   // (else in front of the epilogue)
             } else {
-                load_unit(std::integral_constant<int, P == 1 ? A0 : P == 2 ? B0 : B1>{});
+                if (upper) read_unit(std::integral_constant<int, A1>{}, stage);
+                load_unit(std::integral_constant<int, A0>{}), load_unit(std::integral_constant<int, B0>{}), load_unit(std::integral_constant<int, B1>{});
             }
         };
         if constexpr (P == 1) advance();
         __builtin_amdgcn_sched_barrier(0);
         fetch(lds + c_stage);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (P == 3) {
+        if constexpr (P == 1) {
             if (fresh > 0) stores = 0;
             wait_next();
-        } else if constexpr (P < 2) {
+        } else {
             if (fresh > 0) wait_next();
         }
         __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): what was read here may be overwritten from the next phase on
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
-        constexpr int JB = P == 1 || P == 2 ? 1 : 0, JA = P >= 2 ? 1 : 0;
-        if (JA == 0 || upper)   // nothing to multiply where the tile's rows all lie in A0
+        if (P == 0 || upper)   // nothing to multiply where the tile's rows all lie in A0
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-                for (int q = 0; q < QA; ++q) acc[JB][JA * QA + q] = Half<E>::mfma_32x32x16(JB ? fb1[kk] : fb0[kk], fa[q][kk], acc[JB][JA * QA + q]);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int q = 0; q < QA; ++q) acc[i][P * QA + q] = Half<E>::mfma_32x32x16(i ? fb1[kk] : fb0[kk], fa[q][kk], acc[i][P * QA + q]);
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (STAGGER) {
@@ -255,8 +255,6 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
         for (int s = (t.kv + 63) / 64; s > 0; --s) {
             phase(std::integral_constant<int, 0>{});
             phase(std::integral_constant<int, 1>{});
-            phase(std::integral_constant<int, 2>{});
-            phase(std::integral_constant<int, 3>{});
             fresh = min(fresh + 1, 2);
             c_stage ^= STAGE;
         }
