@@ -106,10 +106,25 @@ __global__ __launch_bounds__(256) void linear_part_sum_kernel(const float *parti
     store4(dw + (size_t)e * size + at, s);
 }
 
-// How the sums of the weights' gradient are cut: not at all where the groups' tiles fill the chip, else into parts that do
+// dx[r] = sum of the parts of row r, in fp32 in their order
+template <typename E>
+__global__ __launch_bounds__(256) void linear_row_sum_kernel(const float *partial, const int32_t *start, E *dx, int N, int rows, int K, int parts)
+{
+    int lo = 0, hi = rows;
+    if (start) lo = min(max(start[0], 0), rows), hi = min(max(start[N], 0), rows);
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4, size = (long long)rows * K;
+    if (at < (long long)lo * K || at >= (long long)hi * K) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) s += *reinterpret_cast<const f32x4 *>(partial + p * size + at);
+    store4(dx + at, s);
+}
+
+// How the gradients' sums are cut: not at all where the tiles fill the chip, else into parts that do.  The parts of both share a piece of the workspace.
 struct GradPlan {
-    int chunk, parts;   // 0: whole groups
-    size_t g_at, sums_at, partial_at, total;
+    int chunk, parts;         // weights: rows of a part (0: whole groups), parts of all groups
+    int x_chunk, x_parts;     // rows: terms of a part, parts
+    size_t sums_at, partial_at, total;
 };
 GradPlan grad_plan(const smile_linear_backward_args &a)
 {
@@ -122,10 +137,21 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
         p.chunk = (int)std::max(256ll, (a.rows / cuts + 63) / 64 * 64);
         p.parts = (a.rows + p.chunk - 1) / p.chunk + a.N - 1;
     }
+    // Parts of at least four slabs; beyond 2^20 rows the tiles alone are more than enough (in bytes the parts are at most 16 times dx of few rows)
+    p.x_parts = 1;
+    const int x_tile = a.dtype == SMILE_DTYPE_F32 ? kF32Tile : 128, slab = 64;
+    const long long x_tiles = std::max(1ll, std::min((long long)a.rows, a.N + a.rows / (long long)x_tile)) * ((a.K + x_tile - 1) / x_tile), slabs = (a.F + slab - 1) / slab;
+    if (a.dx && x_tiles < kLinearCus && slabs >= 8) {
+        const long long parts = std::min(std::min(slabs / 4, 16ll), 2 * kLinearCus / x_tiles);
+        if (parts > 1) {
+            p.x_chunk = (int)((slabs + parts - 1) / parts) * slab;
+            p.x_parts = (a.F + p.x_chunk - 1) / p.x_chunk;
+        }
+    }
     const bool own_g = a.act != SMILE_ACT_NONE && (a.dx || a.dw);
     p.sums_at = round256(own_g ? (size_t)a.rows * a.F * elem_size(a.dtype) : 0);
     p.partial_at = p.sums_at + round256(a.dbias ? ((size_t)(a.rows + kGradRows - 1) / kGradRows + a.N - 1) * a.F * sizeof(float) : 0);
-    p.total = p.partial_at + round256(p.chunk ? (size_t)p.parts * a.F * a.K * sizeof(float) : 0);
+    p.total = p.partial_at + round256(std::max(p.chunk ? (size_t)p.parts * a.F * a.K * sizeof(float) : 0, p.x_parts > 1 ? (size_t)p.x_parts * a.rows * a.K * sizeof(float) : 0));
     return p;
 }
 
@@ -138,7 +164,7 @@ template <typename E, bool GRAD, bool WT>
 hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
 {
     g.col_tiles = (g.Nout + kF32Tile - 1) / kF32Tile, g.row_tiles = (g.Mrows + kF32Tile - 1) / kF32Tile;
-    const long long most = (GRAD ? (long long)g.parts * g.row_tiles : (g.rows + kF32Tile - 1) / kF32Tile + (long long)g.N - 1) * g.col_tiles;
+    const long long most = g.parts * (GRAD ? (long long)g.row_tiles : (g.rows + kF32Tile - 1) / kF32Tile + (long long)std::min(g.N, g.rows) - 1) * g.col_tiles;
     if (most >= 1ll << 31) return hipErrorInvalidValue;
     const int grid = (int)std::min((most + 7) / 8 * 8, (long long)workgroup_slots(tune, 4));
     SMILE_LAUNCH((linear_f32_kernel<E, GRAD, WT>), dim3(grid), dim3(256), 0, s, g);
@@ -150,8 +176,10 @@ hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s
 {
     if constexpr (sizeof(E) == 4) return launch_f32<E, GRAD, WT>(g, tune, s);
     else {
+        const int dtype = std::is_same_v<E, __bf16> ? SMILE_DTYPE_BF16 : SMILE_DTYPE_F16;
+        if (!WT && linear_few_applies(g)) return launch_linear_few(dtype, g, tune, s);
         const LinearKind kind = GRAD ? kLinearWeightGrad : WT ? kLinearRowGrad : kLinearForward;
-        return launch_linear_half(std::is_same_v<E, __bf16> ? SMILE_DTYPE_BF16 : SMILE_DTYPE_F16, g, kind, pick_half_tile(kind, g.N, g.rows, g.Mrows, g.Nout, g.act), tune, s);
+        return launch_linear_half(dtype, g, kind, g.parts > 1 && !GRAD ? kHalf128 : pick_half_tile(kind, g.N, g.rows, g.Mrows, g.Nout, g.act), tune, s);
     }
 }
 
@@ -160,7 +188,7 @@ hipError_t forward(const smile_linear_args &a, const Tuning &tune, hipStream_t s
 {
     LinearGemm g{};
     g.x = a.x, g.w = a.w, g.bias = a.bias, g.residual = a.residual, g.y = a.y, g.pre = a.pre, g.start = a.start;
-    g.N = a.N, g.rows = a.rows, g.Nout = a.F, g.K = a.K, g.ldx = a.K, g.ldw = a.K, g.sw = (long long)a.F * a.K, g.act = act_of(a.act);
+    g.N = a.N, g.rows = a.rows, g.Nout = a.F, g.K = a.K, g.ldx = a.K, g.ldw = a.K, g.sw = (long long)a.F * a.K, g.act = act_of(a.act), g.parts = 1;
     return launch_product<E, false, false>(g, tune, s);
 }
 
@@ -182,9 +210,13 @@ hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, voi
     if (a.dx) {
         LinearGemm m{};
         m.x = g, m.w = a.w, m.y = a.dx, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Nout = a.K, m.K = a.F, m.ldx = a.F, m.ldw = a.K;
-        m.sw = (long long)a.F * a.K;
+        m.sw = (long long)a.F * a.K, m.sy = (long long)a.rows * a.K, m.chunk = p.x_chunk, m.parts = p.x_parts;
+        if (p.x_parts > 1) m.partial = reinterpret_cast<float *>(ws + p.partial_at);
         const hipError_t err = launch_product<E, false, true>(m, tune, s);
         if (err != hipSuccess) return err;
+        if (p.x_parts > 1)
+            SMILE_LAUNCH(linear_row_sum_kernel<E>, dim3((unsigned)((m.sy + 1023) / 1024)), dim3(256), 0, s, (const float *)m.partial, a.start, static_cast<E *>(a.dx), a.N, a.rows,
+                         a.K, p.x_parts);
     }
     if (a.dw) {
         LinearGemm m{};

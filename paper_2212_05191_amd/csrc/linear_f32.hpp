@@ -82,8 +82,8 @@ __global__ __launch_bounds__(256) void linear_f32_kernel(LinearGemm a)
         } else {
             if (!walk.tile(a, n, B, t)) return;
         }
-        const E *X = static_cast<const E *>(a.x) + (GRAD ? (size_t)t.from * a.ldx : (size_t)t.first * a.ldx);
-        const E *W = static_cast<const E *>(a.w) + (GRAD ? (size_t)t.from * a.ldw : (size_t)t.e * a.sw);
+        const E *X = static_cast<const E *>(a.x) + (GRAD ? (size_t)t.from * a.ldx : (size_t)t.first * a.ldx + t.from);
+        const E *W = static_cast<const E *>(a.w) + (GRAD ? 0 : (size_t)t.e * a.sw) + (WT ? (size_t)t.from * a.ldw : t.from);
         Eight<E> xr, wr;
         // this thread's elements of the slab from term k0 on: of an operand whose rows begin at `first` and number `ext`
         auto fetch = [&](Eight<E> &r, const E *p, auto transposed, int ld, int first, int ext, int k0) {
@@ -139,9 +139,10 @@ __global__ __launch_bounds__(256) void linear_f32_kernel(LinearGemm a)
             if (col >= a.Nout) continue;
             f32x4 f = {acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
             const size_t at = (size_t)(t.first + row) * a.Nout + col;
-            if constexpr (GRAD) {
-                if (a.partial) *reinterpret_cast<f32x4 *>(a.partial + (size_t)t.part * a.sy + at) = f;
-                else store4(static_cast<E *>(a.y) + (size_t)t.e * a.sy + at, f);
+            if (WT && a.partial) {
+                *reinterpret_cast<f32x4 *>(a.partial + (size_t)t.part * a.sy + at) = f;
+            } else if constexpr (GRAD) {
+                store4(static_cast<E *>(a.y) + (size_t)t.e * a.sy + at, f);
             } else {
                 if (a.bias) f += load4(static_cast<const E *>(a.bias) + (size_t)t.e * a.Nout + col);
                 if (a.pre) store4(static_cast<E *>(a.pre) + at, f);

@@ -88,8 +88,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
     };
     auto set_sources = [&](const LinearTile &t) __attribute__((always_inline)) {
         l_kv = t.kv, l_slabs = (t.kv + 63) / 64, l_slab = 0;
-        xb = static_cast<const char *>(a.x) + 2 * (size_t)(GRAD ? t.from : t.first) * a.ldx;
-        wb = static_cast<const char *>(a.w) + 2 * (GRAD ? (size_t)t.from * a.ldw : (size_t)t.e * a.sw);
+        xb = static_cast<const char *>(a.x) + 2 * (GRAD ? (size_t)t.from * a.ldx : (size_t)t.first * a.ldx + t.from);
+        wb = static_cast<const char *>(a.w) + 2 * ((GRAD ? 0 : (size_t)t.e * a.sw) + (WT ? (size_t)t.from * a.ldw : t.from));
         const int l = thread_lane();
         for_constants<4>([&](auto type) {
             constexpr int T = decltype(type)::value;
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
         const int ol = thread_lane(), orow = ol & 31, ohi = ol >> 5, col0 = t.col0 + wn * 64;
         if (col0 >= a.Nout) continue;
         auto staged_at = [&](int row, int piece) { return stg + row * 128 + ((piece ^ ((row >> 1) & 7)) * 16); };
-        if (GRAD && a.partial) {
+        if (WT && a.partial) {
             float *P = a.partial + (size_t)t.part * a.sy;
             for_constants<2 * TM>([&](auto block) {
                 constexpr int i = decltype(block)::value % 2, j = decltype(block)::value / 2;
@@ -386,7 +386,7 @@ hipError_t launch_half(LinearGemm g, const Tuning &tune, hipStream_t s)
 {
     constexpr int BM = 64 * QA * WM, BN = 64 * WN, PER_CU = WM * WN == 8 ? 1 : 2;
     g.col_tiles = (g.Nout + BN - 1) / BN, g.row_tiles = (g.Mrows + BM - 1) / BM;
-    const long long most = (GRAD ? (long long)g.parts * g.row_tiles : (g.rows + BM - 1) / BM + (long long)g.N - 1) * g.col_tiles;
+    const long long most = g.parts * (GRAD ? (long long)g.row_tiles : (g.rows + BM - 1) / BM + (long long)std::min(g.N, g.rows) - 1) * g.col_tiles;
     if (most >= 1ll << 31) return hipErrorInvalidValue;
     const int grid = (int)std::min((most + 7) / 8 * 8, (long long)workgroup_slots(tune, PER_CU));
     SMILE_LAUNCH((linear_half_kernel<E, WM, WN, QA, GRAD, WT, ACT>), dim3(grid), dim3(WM * WN * 64), 0, s, g);

@@ -13,13 +13,13 @@ struct LinearGemm {
     const void *bias, *residual;   // [N][Nout], [rows][Nout]
     void *y, *pre;
     const int32_t *start;          // [N+1] or null: one group of all rows
-    float *partial;                // weights' gradient whose sums are cut: [parts][Mrows][Nout]
+    float *partial;                // gradients whose sums are cut into parts: of the weights [parts][Mrows][Nout], of the rows [parts][rows][Nout]; else null
     int N, rows;
     int Mrows, Nout, K;
     int ldx, ldw;                  // elements
-    long long sw, sy;              // elements of a group in w, in y
+    long long sw, sy;              // elements of a group in w; of a group of dw, or of a part
     int row_tiles, col_tiles;      // (row_tiles: weights' gradient)
-    int chunk, parts;              // rows of a part of the sum (0: whole groups), and the parts of all groups
+    int chunk, parts;              // terms of a part of the sum (0: whole sums), and the parts: of all groups (weights' gradient), of a row (rows' gradient)
     int act;                       // 0 none, 1 ReLU, 2 GELU
 };
 
@@ -30,5 +30,9 @@ enum HalfTile { kHalf256, kHalf128 };
 constexpr int kLinearCus = 256;
 HalfTile pick_half_tile(LinearKind kind, int N, int rows, int Mrows, int Nout, int act);
 hipError_t launch_linear_half(int dtype, const LinearGemm &g, LinearKind kind, HalfTile tile, const Tuning &tune, hipStream_t s);
+
+// The forward product of few rows (linear_few.hip), and whether it is the faster one
+hipError_t launch_linear_few(int dtype, const LinearGemm &g, const Tuning &tune, hipStream_t s);
+bool linear_few_applies(const LinearGemm &g);
 
 }  // namespace smile

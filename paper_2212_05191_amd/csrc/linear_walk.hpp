@@ -39,7 +39,7 @@ template <int BM, int BAND>
 struct RowWalk {
     const int32_t *start;
     int N, rows, col_tiles, lane;
-    int chunk_incl, cur_chunk, cur_incl, tickets;
+    int chunk_incl, cur_chunk, cur_incl, whole, tickets;   // whole: tiles of one part of the sums
 
     __device__ __forceinline__ int tiles_of(int g) const
     {
@@ -68,14 +68,17 @@ struct RowWalk {
             }
             chunk_incl = LiveTileWalk<1>::scan(mine);
         }
-        tickets = __builtin_amdgcn_readlane(chunk_incl, 63) * col_tiles;
+        whole = __builtin_amdgcn_readlane(chunk_incl, 63) * col_tiles;
+        tickets = whole * a.parts;
     }
     // the n-th tile of this workgroup; false behind its last
     __device__ __forceinline__ bool tile(const LinearGemm &a, int n, int tile_cols, LinearTile &t)
     {
         const int each = (tickets + 7) / 8, local = blockIdx.x / 8 + n * (gridDim.x / 8);
-        const int ticket = (blockIdx.x % 8) * each + local;
+        int ticket = (blockIdx.x % 8) * each + local;
         if (local >= each || ticket >= tickets) return false;
+        t.part = a.parts > 1 ? ticket / whole : 0;
+        ticket -= t.part * whole;
         const int I = ticket / col_tiles;
         const int c = __builtin_ctzll(__ballot(chunk_incl > I));
         const int before = c ? __builtin_amdgcn_readlane(chunk_incl, c - 1) : 0;
@@ -90,7 +93,7 @@ struct RowWalk {
         t.e = c * 64 + l;
         group_rows(start, rows, t.e, lo, hi);
         t.first = lo + rt * BM, t.rows = hi - t.first, t.col0 = ct * tile_cols;
-        t.from = 0, t.kv = a.K, t.part = 0;
+        t.from = t.part * a.chunk, t.kv = a.parts > 1 ? min(a.chunk, a.K - t.from) : a.K;
         return true;
     }
 };
