@@ -8,12 +8,16 @@
 #include "sorted_internal.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace smile {
 
 namespace {
 
 constexpr int kThreads = 256, kEach = kAdamwChunk / kThreads;
+// Workgroups on a CU, all resident: a thread has one chunk's loads in flight, so their number is what covers the memory's latency.  134 M elements with 8-bit states and
+// master weights, without and with the codes past the L2: five (88 registers) 554 / 532 us, six 514 / 490, seven (72 registers) 467, eight spill 535.
+constexpr int kPerCu = 7;
 static_assert(kEach == 8, "eight elements a thread");
 
 // A 32-bit integer hash: xor-shifts and multiplications
@@ -38,32 +42,24 @@ __device__ __forceinline__ double one_minus_power(double beta, uint32_t t)
 }
 
 // the largest of the 16 lanes of a block
-__device__ __forceinline__ float block_max(float v)
+__device__ __forceinline__ uint32_t block_max(uint32_t v)
 {
-    auto step = [&](int other) { v = fmaxf(v, __int_as_float(other)); };
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true));
-    return v;
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));
 }
 
-__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+constexpr uint32_t kInfinity = 0x7f800000u;   // magnitudes from here on are not finite
 
 // ---- the first moment: e4m3 codes.  Between two codes of a value's binade lie 2^20 steps of fp32, of which the 16 random bits are the upper ones: adding
-// them to the float's bits and cutting off 20 rounds up where the part cut off is at least 1 - R / 65536 of a code's step, and carries into the exponent.
+// them to the float's bits and cutting off 20 rounds up where the part cut off is at least 1 - R / 65536 of a code's step, and carries into the exponent.  Below 2^-6 the
+// codes are 2^-9 apart: the same in units of 2^-25.  v finite.
 __device__ __forceinline__ uint32_t m_code(float v, int e, uint32_t r)   // e: exponent of the block's power of two
 {
-    if (!finite(v)) return 0x7fu;
     const float u = __builtin_amdgcn_ldexpf(fabsf(v), -e);
-    uint32_t c;
-    if (u >= 0.015625f) {                                   // 2^-6, the least normal code
-        c = ((__float_as_uint(u) + (r << 4)) >> 20) - ((127u - 7u) << 3);
-    } else {
-        const float a = u * 512.f, whole = floorf(a);       // steps of 2^-9
-        c = (uint32_t)whole + (a - whole >= 1.f - (float)r * (1.f / 65536.f) ? 1u : 0u);
-    }
-    return c | (__float_as_uint(v) >> 31 << 7);
+    const uint32_t normal = ((__float_as_uint(u) + (r << 4)) >> 20) - ((127u - 7u) << 3), small = ((uint32_t)(u * 33554432.f) + r) >> 16;
+    return (u >= 0.015625f ? normal : small) | (__float_as_uint(v) >> 24 & 0x80u);
 }
 // exponent of the block's power of two: the least with which `largest` is at most 448 = 0.875 * 2^9
 __device__ __forceinline__ int m_exponent(float largest)
@@ -73,57 +69,58 @@ __device__ __forceinline__ int m_exponent(float largest)
     return max(__builtin_amdgcn_frexp_expf(largest) - 9 + (f > 0.875f ? 1 : 0), -126);
 }
 
-// ---- the second moment: codes of 5 exponent and 3 fraction bits, code 8 (x + 30) + f for (1 + f / 8) 2^x of the block's power of two
+// ---- the second moment: codes of 5 exponent and 3 fraction bits, code 8 (x + 30) + f for (1 + f / 8) 2^x of the block's power of two.  v finite.
 __device__ __forceinline__ uint32_t v_code(float v, int e, uint32_t r)
 {
-    if (!finite(v)) return 0xffu;
-    if (v == 0.f) return 0u;
     const float u = __builtin_amdgcn_ldexpf(v, -e);         // below 2; what is so small that it loses bits here gets the least code
     const int c = (int)((__float_as_uint(u) + (r << 4)) >> 20) - ((127 - 30) << 3);
-    return (uint32_t)max(c, 1);
+    return v == 0.f ? 0u : (uint32_t)max(c, 1);
 }
 __device__ __forceinline__ int v_exponent(float largest)
 {
     return largest == 0.f ? -126 : max(__builtin_amdgcn_frexp_expf(largest) - 1, -126);
 }
-__device__ __forceinline__ float v_value(uint32_t c, int e)
-{
-    return c == 0 ? 0.f : __builtin_amdgcn_ldexpf(__uint_as_float((c + ((127u - 30u) << 3)) << 20), e);
-}
 
-__device__ __forceinline__ void m_values(uint2 codes, int e, float *m)
-{
-    unpack4(codes.x, 1.f, m), unpack4(codes.y, 1.f, m + 4);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m[i] = __builtin_amdgcn_ldexpf(m[i], e);
-}
-__device__ __forceinline__ void v_values(uint2 codes, int e, float *v)
+// values of eight codes, before the block's power of two; and after
+__device__ __forceinline__ void m_units(uint2 codes, float *m) { unpack4(codes.x, 1.f, m), unpack4(codes.y, 1.f, m + 4); }
+__device__ __forceinline__ float v_unit(uint32_t c) { return c == 0 ? 0.f : __uint_as_float((c + ((127u - 30u) << 3)) << 20); }
+__device__ __forceinline__ void v_units(uint2 codes, float *v)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = v_value(codes.x >> 8 * i & 255u, e), v[4 + i] = v_value(codes.y >> 8 * i & 255u, e);
+    for (int i = 0; i < 4; ++i) v[i] = v_unit(codes.x >> 8 * i & 255u), v[4 + i] = v_unit(codes.y >> 8 * i & 255u);
+}
+__device__ __forceinline__ void scaled(float *v, int e)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], e);
 }
 
-// Eight neighbouring elements: all of them in 16-byte pieces, or the first `live`
+// the first `live` of eight neighbouring elements, zeros behind them
 template <int DT>
-__device__ __forceinline__ void load8(const void *base, size_t at, int live, float *v)
+__device__ __forceinline__ void load_some(const void *base, size_t at, int live, float *v)
 {
-    if (live >= 8) {
-        Piece<DT>::widen(Piece<DT>::load(base, at), v);
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < live ? (float)static_cast<const typename Piece<DT>::E *>(base)[at + i] : 0.f;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = i < live ? (float)static_cast<const typename Piece<DT>::E *>(base)[at + i] : 0.f;
 }
 template <int DT>
 __device__ __forceinline__ void store8(void *base, size_t at, int live, const float *v)
 {
     if (live >= 8) {
-        Piece<DT>::store(base, at, Piece<DT>::narrow(v));
+        // not read again by this launch: past the L2 (134 M elements, 8-bit states: 568 -> 545 us)
+        const auto r = Piece<DT>::narrow(v);
+        u32x4 *p = reinterpret_cast<u32x4 *>(static_cast<typename Piece<DT>::E *>(base) + at);
+        __builtin_nontemporal_store(r.a, p);
+        if constexpr (DT == SMILE_DTYPE_F32) __builtin_nontemporal_store(r.b, p + 1);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < live) static_cast<typename Piece<DT>::E *>(base)[at + i] = (typename Piece<DT>::E)v[i];
     }
+}
+
+__device__ __forceinline__ void store_codes(void *base, size_t at, const uint32_t (&c)[2])
+{
+    __builtin_nontemporal_store((uint64_t)c[1] << 32 | c[0], reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(base) + at));
 }
 
 struct AdamwStep {
@@ -139,7 +136,7 @@ struct AdamwStep {
 };
 
 template <int DT, int GDT, bool EIGHT, bool MASTER>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwStep a)
+__global__ __launch_bounds__(kThreads, kPerCu) void adamw_kernel(AdamwStep a)
 {
     AdamwChunk c = a.list[blockIdx.x];
     const float lr = *a.lr;
@@ -152,64 +149,112 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwStep a)
         atomicExch(a.arrived, 0);
         *a.step = (int32_t)t;
     }
-    const float inv1 = (float)(1.0 / one_minus_power(a.beta1, t)), inv2 = (float)(1.0 / one_minus_power(a.beta2, t));
     const uint32_t key_step = mix(mix(a.seed) ^ t);
-    for (long long n = blockIdx.x; n < a.chunks; n += gridDim.x) {
-        if (n != blockIdx.x) c = a.list[n];
+    // one chunk's loads are in flight while the one before is computed and stored
+    struct Raw {
+        typename Piece<GDT>::Raw g;
+        typename Piece<MASTER ? SMILE_DTYPE_F32 : DT>::Raw p;
+        typename std::conditional_t<EIGHT, uint2, typename Piece<SMILE_DTYPE_F32>::Raw> m, v;
+        uint8_t m_scale, v_scale;
+    };
+    auto fetch = [&](AdamwChunk c, Raw &r) {
         const AdamwTensor &x = a.tensors[c.tensor];
         const size_t at = (size_t)c.chunk * kAdamwChunk + threadIdx.x * 8;
-        const long long left = x.n - (long long)at;
-        const int live = (int)min(left, 8ll);
-        // (8-bit states: the lanes of a block that holds an element stay together, behind the tensor's end too)
-        if (EIGHT ? (long long)at >= (x.n + 127) / 128 * 128 : live <= 0) continue;
-        float g[8], p[8], m[8], v[8];
-        const size_t block = at / 128;
-        load8<GDT>(x.grad, at, live, g);
-        if constexpr (MASTER) load8<SMILE_DTYPE_F32>(x.master, at, live, p);
-        else load8<DT>(x.param, at, live, p);
+        if ((long long)at + 8 <= x.n) {
+            r.g = Piece<GDT>::load(x.grad, at);
+            r.p = Piece<MASTER ? SMILE_DTYPE_F32 : DT>::load(MASTER ? x.master : x.param, at);
+            if constexpr (!EIGHT) r.m = Piece<SMILE_DTYPE_F32>::load(x.m, at), r.v = Piece<SMILE_DTYPE_F32>::load(x.v, at);
+        }
         if constexpr (EIGHT) {
-            const uint2 mc = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(x.m) + at);
-            const uint2 vc = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(x.v) + at);
-            m_values(mc, (int)x.m_scale[block] - 127, m);
-            v_values(vc, (int)x.v_scale[block] - 127, v);
-        } else {
-            load8<SMILE_DTYPE_F32>(x.m, at, live, m);
-            load8<SMILE_DTYPE_F32>(x.v, at, live, v);
+            if ((long long)at < (x.n + 127) / 128 * 128) {
+                r.m = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(x.m) + at), r.v = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(x.v) + at);
+                r.m_scale = x.m_scale[at / 128], r.v_scale = x.v_scale[at / 128];
+            }
         }
-        const float decay = x.weight_decay;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i] = fmaf(a.beta1_f, m[i], a.rest1 * g[i]);
-            v[i] = fmaf(a.beta2_f, v[i], a.rest2 * g[i] * g[i]);
-            const float update = m[i] * inv1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inv2) + a.eps);
-            p[i] -= lr * fmaf(decay, p[i], update);
+    };
+    Raw cur, nxt;
+    fetch(c, cur);
+    const float inv1 = (float)(1.0 / one_minus_power(a.beta1, t)), inv2 = (float)(1.0 / one_minus_power(a.beta2, t));
+    for (long long n = blockIdx.x; n < a.chunks; n += gridDim.x) {
+        AdamwChunk ahead = c;
+        if (n + gridDim.x < a.chunks) {
+            ahead = a.list[n + gridDim.x];
+            fetch(ahead, nxt);
         }
-        store8<DT>(x.param, at, live, p);
-        if constexpr (MASTER) store8<SMILE_DTYPE_F32>(x.master, at, live, p);
-        if constexpr (!EIGHT) {
-            store8<SMILE_DTYPE_F32>(x.m, at, live, m);
-            store8<SMILE_DTYPE_F32>(x.v, at, live, v);
-        } else {
-            float top_m = 0.f, top_v = 0.f;
+        const AdamwTensor &x = a.tensors[c.tensor];
+        const size_t at = (size_t)c.chunk * kAdamwChunk + threadIdx.x * 8;
+        const int live = (int)min(x.n - (long long)at, 8ll);
+        // (8-bit states: the lanes of a block that holds an element stay together, behind the tensor's end too)
+        if (EIGHT ? (long long)at < (x.n + 127) / 128 * 128 : live > 0) {
+            float g[8], p[8], m[8], v[8];
+            if (live == 8) {
+                Piece<GDT>::widen(cur.g, g);
+                Piece<MASTER ? SMILE_DTYPE_F32 : DT>::widen(cur.p, p);
+                if constexpr (!EIGHT) Piece<SMILE_DTYPE_F32>::widen(cur.m, m), Piece<SMILE_DTYPE_F32>::widen(cur.v, v);
+            } else {
+                load_some<GDT>(x.grad, at, live, g);
+                load_some<MASTER ? SMILE_DTYPE_F32 : DT>(MASTER ? x.master : x.param, at, live, p);
+                if constexpr (!EIGHT) load_some<SMILE_DTYPE_F32>(x.m, at, live, m), load_some<SMILE_DTYPE_F32>(x.v, at, live, v);
+            }
+            if constexpr (EIGHT) {
+                m_units(cur.m, m), scaled(m, (int)cur.m_scale - 127);
+                v_units(cur.v, v), scaled(v, (int)cur.v_scale - 127);
+            }
+            const float decay = x.weight_decay;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (i >= live) m[i] = v[i] = 0.f;
-                if (finite(m[i])) top_m = fmaxf(top_m, fabsf(m[i]));
-                if (finite(v[i])) top_v = fmaxf(top_v, v[i]);
+                m[i] = fmaf(a.beta1_f, m[i], a.rest1 * g[i]);
+                v[i] = fmaf(a.beta2_f, v[i], a.rest2 * g[i] * g[i]);
+                const float update = m[i] * inv1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inv2) + a.eps);
+                p[i] -= lr * fmaf(decay, p[i], update);
             }
-            const int em = m_exponent(block_max(top_m)), ev = v_exponent(block_max(top_v));
-            const uint32_t key = mix(key_step ^ (uint32_t)c.tensor);
-            uint32_t mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
+            store8<DT>(x.param, at, live, p);
+            if constexpr (MASTER) store8<SMILE_DTYPE_F32>(x.master, at, live, p);
+            if constexpr (!EIGHT) {
+                store8<SMILE_DTYPE_F32>(x.m, at, live, m);
+                store8<SMILE_DTYPE_F32>(x.v, at, live, v);
+            } else {
+                uint32_t top_m = 0u, top_v = 0u;   // largest magnitudes, which as bits have the order of their values
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t r = mix((uint32_t)at + i + key);
-                mc[i / 4] |= m_code(m[i], em, r & 0xffffu) << 8 * (i % 4);
-                vc[i / 4] |= v_code(v[i], ev, r >> 16) << 8 * (i % 4);
+                for (int i = 0; i < 8; ++i) {
+                    if (i >= live) m[i] = v[i] = 0.f;
+                    top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu), top_v = max(top_v, __float_as_uint(v[i]) & 0x7fffffffu);
+                }
+                top_m = block_max(top_m), top_v = block_max(top_v);
+                uint32_t odd = 0u;                 // elements of a gradient that is not finite: their codes are set below
+                if (max(top_m, top_v) >= kInfinity) {
+                    top_m = top_v = 0u;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t mm = __float_as_uint(m[i]) & 0x7fffffffu, vv = __float_as_uint(v[i]) & 0x7fffffffu;
+                        if (mm >= kInfinity) odd |= 1u << i, m[i] = 0.f;
+                        else top_m = max(top_m, mm);
+                        if (vv >= kInfinity) odd |= 256u << i, v[i] = 0.f;
+                        else top_v = max(top_v, vv);
+                    }
+                    top_m = block_max(top_m), top_v = block_max(top_v);
+                }
+                const int em = m_exponent(__uint_as_float(top_m)), ev = v_exponent(__uint_as_float(top_v));
+                const uint32_t key = mix(key_step ^ (uint32_t)c.tensor) + (uint32_t)at;
+                uint32_t mc[2] = {0u, 0u}, vc[2] = {0u, 0u};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t r = mix(key + i);
+                    mc[i / 4] |= m_code(m[i], em, r & 0xffffu) << 8 * (i % 4);
+                    vc[i / 4] |= v_code(v[i], ev, r >> 16) << 8 * (i % 4);
+                }
+                if (odd)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (odd >> i & 1u) mc[i / 4] |= 0x7fu << 8 * (i % 4);
+                        if (odd >> i & 256u) vc[i / 4] |= 0xffu << 8 * (i % 4);
+                    }
+                store_codes(x.m, at, mc);
+                store_codes(x.v, at, vc);
+                if ((threadIdx.x & 15) == 0) x.m_scale[at / 128] = (uint8_t)(em + 127), x.v_scale[at / 128] = (uint8_t)(ev + 127);
             }
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(x.m) + at) = uint2{mc[0], mc[1]};
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(x.v) + at) = uint2{vc[0], vc[1]};
-            if ((threadIdx.x & 15) == 0) x.m_scale[block] = (uint8_t)(em + 127), x.v_scale[block] = (uint8_t)(ev + 127);
         }
+        cur = nxt, c = ahead;
     }
 }
 
@@ -220,9 +265,9 @@ __global__ __launch_bounds__(kThreads) void adamw_unpack_kernel(long long n, con
     const long long stride = (long long)gridDim.x * kAdamwChunk;
     for (long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) * 8; at < n; at += stride) {
         float f[8];
-        m_values(*reinterpret_cast<const uint2 *>(m + at), (int)m_scale[at / 128] - 127, f);
+        m_units(*reinterpret_cast<const uint2 *>(m + at), f), scaled(f, (int)m_scale[at / 128] - 127);
         store8<DT>(m_value, at, 8, f);
-        v_values(*reinterpret_cast<const uint2 *>(v + at), (int)v_scale[at / 128] - 127, f);
+        v_units(*reinterpret_cast<const uint2 *>(v + at), f), scaled(f, (int)v_scale[at / 128] - 127);
         store8<DT>(v_value, at, 8, f);
     }
 }
@@ -253,7 +298,7 @@ hipError_t launch_adamw(const smile_adamw_args &a, void *plan, const float *lr, 
     st.list = reinterpret_cast<const AdamwChunk *>(base + kAdamwTensorsAt + (size_t)a.tensors * sizeof(AdamwTensor));
     st.lr = lr, st.step = step, st.chunks = a.chunks, st.beta1 = a.beta1, st.beta2 = a.beta2, st.seed = (uint32_t)a.seed;
     st.beta1_f = (float)a.beta1, st.beta2_f = (float)a.beta2, st.rest1 = (float)(1.0 - a.beta1), st.rest2 = (float)(1.0 - a.beta2), st.eps = (float)a.eps;
-    const int grid = (int)std::min((long long)a.chunks, (long long)workgroup_slots(tune, 8));
+    const int grid = (int)std::min((long long)a.chunks, (long long)workgroup_slots(tune, kPerCu));
     constexpr int F = SMILE_DTYPE_F32, B = SMILE_DTYPE_BF16, H = SMILE_DTYPE_F16;
     if (a.dtype == F) return launch_typed<F, F>(a, st, grid, s);
     if (a.dtype == B) return a.grad_dtype == F ? launch_typed<B, F>(a, st, grid, s) : launch_typed<B, B>(a, st, grid, s);
