@@ -120,32 +120,57 @@ __global__ __launch_bounds__(256) void linear_row_sum_kernel(const float *partia
     store4(dx + at, s);
 }
 
-// How the gradients' sums are cut: not at all where the tiles fill the chip, else into parts that do.  The parts of both share a piece of the workspace.
+// How the gradients' sums are cut into parts, where their tiles leave the chip idle: the tile and the number of parts with the least estimated time, of which a part
+// costs a launch and its bytes, written and read in fp32 (at 9 TB/s: they mostly stay in the caches).  The parts of both gradients share a piece of the workspace.
 struct GradPlan {
     int chunk, parts;         // weights: rows of a part (0: whole groups), parts of all groups
     int x_chunk, x_parts;     // rows: terms of a part, parts
+    HalfTile tile;            // weights, 16-bit types
     size_t sums_at, partial_at, total;
 };
+constexpr int kMostParts = 16;
+double parts_time(int parts, double elements) { return parts > 1 ? 4.0 + parts * elements * 8.0 / 9e6 : 0.0; }
+
 GradPlan grad_plan(const smile_linear_backward_args &a)
 {
     GradPlan p{};
-    p.parts = a.N;
-    const int tile = a.dtype == SMILE_DTYPE_F32 ? kF32Tile : pick_half_tile(kLinearWeightGrad, a.N, a.rows, a.F, a.K, 0) == kHalf256 ? 256 : 128;
-    const long long tiles = (long long)a.N * ((a.F + tile - 1) / tile) * ((a.K + tile - 1) / tile), want = tile == 256 ? kLinearCus : 2 * kLinearCus;
-    if (a.dw && tiles < want && a.rows > 256) {
-        const long long cuts = (want + tiles - 1) / tiles * a.N;   // parts of all groups, if they are alike
-        p.chunk = (int)std::max(256ll, (a.rows / cuts + 63) / 64 * 64);
-        p.parts = (a.rows + p.chunk - 1) / p.chunk + a.N - 1;
+    const bool half = a.dtype != SMILE_DTYPE_F32;
+    // an fp32 tile of 64 x 64 outputs takes about as long for a slab of 64 terms, four of them on a CU, as one of 128 x 128 in 16 bits
+    auto time = [&](int size, double tiles, double slabs) {
+        return half ? linear_half_time(size == 256 ? kHalf256 : kHalf128, tiles, slabs, false) : linear_half_time(kHalf128, tiles / 2, 1.5 * slabs, false);
+    };
+    auto tiles_of = [](int n, int size) { return (n + size - 1) / size; };
+    p.parts = a.N, p.tile = kHalf128;
+    if (a.dw) {
+        const double elements = (double)a.N * a.F * a.K;
+        double best = 1e30;
+        int cuts = 1;
+        for (const int size : {half ? 128 : kF32Tile, 256}) {
+            if (!half && size == 256) break;
+            for (int n = 1; n <= kMostParts && (n == 1 || (long long)a.N * n * 256 <= a.rows); ++n) {
+                const double per_group = std::ceil((double)a.rows / a.N / n / 64);
+                const double t = time(size, (double)a.N * n * tiles_of(a.F, size) * tiles_of(a.K, size), per_group) + parts_time(n, elements);
+                if (t < best) best = t, cuts = n, p.tile = size == 256 ? kHalf256 : kHalf128;
+            }
+        }
+        if (cuts > 1) {
+            p.chunk = (int)std::max(64ll, ((long long)a.rows / a.N / cuts + 63) / 64 * 64);
+            p.parts = tiles_of(a.rows, p.chunk) + a.N - 1;
+        }
     }
-    // Parts of at least four slabs; beyond 2^20 rows the tiles alone are more than enough (in bytes the parts are at most 16 times dx of few rows)
     p.x_parts = 1;
-    const int x_tile = a.dtype == SMILE_DTYPE_F32 ? kF32Tile : 128, slab = 64;
-    const long long x_tiles = std::max(1ll, std::min((long long)a.rows, a.N + a.rows / (long long)x_tile)) * ((a.K + x_tile - 1) / x_tile), slabs = (a.F + slab - 1) / slab;
-    if (a.dx && x_tiles < kLinearCus && slabs >= 8) {
-        const long long parts = std::min(std::min(slabs / 4, 16ll), 2 * kLinearCus / x_tiles);
-        if (parts > 1) {
-            p.x_chunk = (int)((slabs + parts - 1) / parts) * slab;
-            p.x_parts = (a.F + p.x_chunk - 1) / p.x_chunk;
+    if (a.dx) {
+        const int size = half ? 128 : kF32Tile, slabs = tiles_of(a.F, 64);
+        const double per = (double)a.rows / a.N, tiles = (a.N == 1 ? std::ceil(per / size) : std::min((double)a.rows, a.N * std::max(1.0, per / size + 0.5))) * tiles_of(a.K, size);
+        double best = time(size, tiles, slabs);
+        int cuts = 1;
+        for (int n = 2; n <= kMostParts && 4 * n <= slabs; ++n) {
+            const double t = time(size, tiles * n, tiles_of(slabs, n)) + parts_time(n, (double)a.rows * a.K);
+            if (t < best) best = t, cuts = n;
+        }
+        if (cuts > 1) {
+            p.x_chunk = tiles_of(slabs, cuts) * 64;
+            p.x_parts = tiles_of(a.F, p.x_chunk);
         }
     }
     const bool own_g = a.act != SMILE_ACT_NONE && (a.dx || a.dw);
@@ -156,9 +181,6 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
 }
 
 int act_of(int act) { return act == SMILE_ACT_NONE ? 0 : act == SMILE_ACT_RELU ? 1 : 2; }
-
-template <typename E, bool GRAD, bool WT>
-hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s);
 
 template <typename E, bool GRAD, bool WT>
 hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
@@ -172,14 +194,14 @@ hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
 }
 
 template <typename E, bool GRAD, bool WT>
-hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s)
+hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s, const HalfTile *tile = nullptr)
 {
     if constexpr (sizeof(E) == 4) return launch_f32<E, GRAD, WT>(g, tune, s);
     else {
         const int dtype = std::is_same_v<E, __bf16> ? SMILE_DTYPE_BF16 : SMILE_DTYPE_F16;
         if (!WT && linear_few_applies(g)) return launch_linear_few(dtype, g, tune, s);
         const LinearKind kind = GRAD ? kLinearWeightGrad : WT ? kLinearRowGrad : kLinearForward;
-        return launch_linear_half(dtype, g, kind, g.parts > 1 && !GRAD ? kHalf128 : pick_half_tile(kind, g.N, g.rows, g.Mrows, g.Nout, g.act), tune, s);
+        return launch_linear_half(dtype, g, kind, tile ? *tile : pick_half_tile(kind, g), tune, s);
     }
 }
 
@@ -223,7 +245,7 @@ hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, voi
         m.x = g, m.w = a.x, m.y = a.dw, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Mrows = a.F, m.Nout = a.K, m.ldx = a.F, m.ldw = a.K;
         m.sy = (long long)a.F * a.K, m.chunk = p.chunk, m.parts = p.parts;
         if (p.chunk) m.partial = reinterpret_cast<float *>(ws + p.partial_at);
-        const hipError_t err = launch_product<E, true, true>(m, tune, s);
+        const hipError_t err = launch_product<E, true, true>(m, tune, s, &p.tile);
         if (err != hipSuccess) return err;
         if (p.chunk)
             SMILE_LAUNCH(linear_part_sum_kernel<E>, dim3((unsigned)((m.sy + 1023) / 1024), a.N), dim3(256), 0, s, (const float *)m.partial, a.start, static_cast<E *>(a.dw),

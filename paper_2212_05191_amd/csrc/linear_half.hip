@@ -26,37 +26,33 @@ hipError_t launch_typed(const LinearGemm &g, LinearKind kind, HalfTile tile, con
     return launch_shape<E, 2, 2, 1>(g, kind, tune, s);
 }
 
-// Time of `tiles` tiles in rounds of the chip, a round of 256 x 256 tiles being 1 (and of 128 x 128 tiles `weight`, a little more than half of that if half of
-// the slots are empty); from three rounds on workgroups are out of step and share the last one.
-double rounds(double tiles, int slots, double weight, double half)
-{
-    const double n = tiles / slots;
-    if (n > 3.0) return weight * (n + 0.25);
-    const double whole = std::floor(n), rest = n - whole;
-    return weight * whole + (rest <= 0.0 ? 0.0 : rest <= 0.5 ? half : weight);
-}
-
 }  // namespace
 
 // 256 x 256 outputs alone on a CU move half of the bytes from L2 that 128 x 128 do, but the epilogue waits for nobody and nobody multiplies meanwhile, and there
-// are a quarter as many tiles to spread.  Measured, us, 256 and 128 (bfloat16, two cards, of which the second runs at a lower clock):
-//   forward, 16384 rows 4096 -> 1024: 119 / 135 and 143 / 155; 64 groups of 512 rows, 1024 -> 4096: 337 / 363, 391 / 398; with GELU 420 / 402 and 467 / 435
-//   gradient of x, 16384 rows 4096 -> 1024: 150 / 167, 170 / 200; of the weights, 64 groups: 387 / 451, 398 / 460
-//   4096 rows 1024 -> 1024 (64 and 256 tiles): 30 / 15; 16 groups of 512 rows 768 -> 2304 with GELU: 66 / 44
-// so that a round of two 128 x 128 tiles on each CU counts as 0.56 of one of 256 x 256, with GELU as 0.48.  Groups of unknown rows are taken as even, with half a
-// tile more each.
-HalfTile pick_half_tile(LinearKind kind, int N, int rows, int Mrows, int Nout, int act)
+// are a quarter as many tiles to spread.  Time of `tiles` tiles of `slabs` slabs, us: rounds of the chip, each slabs x time of a slab + what a tile costs beside it; from
+// three rounds on workgroups are out of step and share the last one.  Its figures, and what they stand for (bfloat16; measured, 256 and 128, in brackets the model):
+//   forward, 16384 rows 4096 -> 1024: 143 / 155 (135 / 147); 64 groups of 512 rows, 1024 -> 4096: 391 / 398 (399 / 407), with GELU 470 / 435 (497 / 461)
+//   gradient of x, 16384 rows 4096 -> 1024: 171 / 200 (168 / 187); of the weights, 64 groups: 395 / 460 (380 / 441)
+//   4096 rows 1024 -> 1024 (64 and 256 tiles): 30 / 19 (43 / 19); 16 groups of 512 rows 768 -> 2304 with GELU: 66 / 50 (85 / 67)
+double linear_half_time(HalfTile tile, double tiles, double slabs, bool gelu)
 {
-    auto tiles = [&](int size) {
-        const double cols = (Nout + size - 1) / size, per = (double)rows / N;
-        if (kind == kLinearWeightGrad) return (double)N * ((Mrows + size - 1) / size) * cols;
-        return N == 1 ? std::ceil(per / size) * cols : (per < 1.0 ? rows : N * std::max(1.0, per / size + 0.5)) * cols;
+    auto shared = [](double n) { return n <= 3.0 ? std::ceil(n) : n + 0.25; };
+    if (tile == kHalf256) return 5.0 + shared(tiles / kLinearCus) * (1.9 * slabs + (gelu ? 17.5 : 8.0));
+    const double n = tiles / (2 * kLinearCus), beside = gelu ? 8.0 : 5.0;
+    return 5.0 + (n <= 0.5 ? 0.68 * slabs + 0.6 * beside : shared(n) * (1.06 * slabs + beside));
+}
+
+// Groups of unknown rows are taken as even, with half a tile more each
+HalfTile pick_half_tile(LinearKind kind, const LinearGemm &g)
+{
+    auto time = [&](HalfTile tile) {
+        const int size = tile == kHalf256 ? 256 : 128;
+        const double cols = (g.Nout + size - 1) / size, per = (double)g.rows / g.N;
+        if (kind == kLinearWeightGrad) return linear_half_time(tile, (double)g.parts * ((g.Mrows + size - 1) / size) * cols, std::ceil((double)g.rows / g.parts / 64), false);
+        const double tiles = g.N == 1 ? std::ceil(per / size) : std::min((double)g.rows, g.N * std::max(1.0, per / size + 0.5));
+        return linear_half_time(tile, g.parts * tiles * cols, std::ceil((double)g.K / g.parts / 64), g.act == 2);
     };
-    const double big = tiles(256), small = tiles(128), weight = act == 2 ? 0.48 : 0.56;
-    if (kind == kLinearWeightGrad && N * (long long)rows > 0) {   // few tiles: the sums are cut until the chip is full
-        if (big < kLinearCus && small < 2 * kLinearCus) return rows >= 8192 && big >= 16 ? kHalf256 : kHalf128;
-    }
-    return rounds(big, kLinearCus, 1.0, 1.0) <= rounds(small, 2 * kLinearCus, weight, 0.7 * weight) ? kHalf256 : kHalf128;
+    return time(kHalf256) <= time(kHalf128) ? kHalf256 : kHalf128;
 }
 
 hipError_t launch_linear_half(int dtype, const LinearGemm &g, LinearKind kind, HalfTile tile, const Tuning &tune, hipStream_t s)

@@ -26,9 +26,10 @@ struct LinearGemm {
 enum LinearKind { kLinearForward, kLinearRowGrad, kLinearWeightGrad };
 // Tiles of the 16-bit kernel: 256 x 256 alone on a CU, 128 x 128 two on a CU
 enum HalfTile { kHalf256, kHalf128 };
-// what the choice of a tile and the split of the weights' gradient go by: the latter's workspace is asked for on the host alone
+// what the choice of a tile and the cuts of the gradients' sums go by: their workspace is asked for on the host alone
 constexpr int kLinearCus = 256;
-HalfTile pick_half_tile(LinearKind kind, int N, int rows, int Mrows, int Nout, int act);
+HalfTile pick_half_tile(LinearKind kind, const LinearGemm &g);
+double linear_half_time(HalfTile tile, double tiles, double slabs, bool gelu);   // estimated, us
 hipError_t launch_linear_half(int dtype, const LinearGemm &g, LinearKind kind, HalfTile tile, const Tuning &tune, hipStream_t s);
 
 // The forward product of few rows (linear_few.hip), and whether it is the faster one

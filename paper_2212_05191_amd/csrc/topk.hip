@@ -2,9 +2,9 @@
 // gradient of the logits.
 //
 // A token is L lanes of a wave, each with V of its values in registers (column 4 (i L + lane) + q, 16 bytes at a time), so that a row is
-// read once and nothing of it is kept anywhere else.  A choice takes the maximum over the lane's values (two a v_max3), over the lanes by
-// DPP, the first column that holds it, and removes that one.  Bound: HBM for many tokens (4 N bytes read each, and 4 N written by
-// the gradient); by instructions where k is large (4.5 V a choice); by latency for few tokens.
+// read once and nothing of it is kept anywhere else.  A choice takes the largest of the lane's values, each with its column
+// one double, then of the lanes by DPP, and removes it.  Bound: HBM for many tokens (4 N bytes read each, and 4 N written by
+// the gradient); by instructions where k is large (3 V a choice); by latency for few tokens.
 #include "gemm_device.hpp"
 #include "sorted_internal.hpp"
 
@@ -14,7 +14,8 @@ namespace smile {
 
 namespace {
 
-constexpr int kThreads = 256, kMaxBlocks = 512;
+// Workgroups of the choice: more of them make more partial sums, fewer leave the CUs short of waves (65536 x 128, k = 8: 512 31 us, 1024 25, 2048 25 and a longer sum)
+constexpr int kThreads = 256, kMaxBlocks = 1024;
 // tokens that one workgroup takes alone, without a second launch for p_sum: lanes of work
 constexpr int kAloneLanes = 4 * kThreads;
 
@@ -36,8 +37,6 @@ __device__ __forceinline__ T over_lanes(T v, F f)
 template <int L>
 __device__ __forceinline__ float max_over(float v) { return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
 template <int L>
-__device__ __forceinline__ int min_over(int v) { return over_lanes<L>(v, [](int a, int b) { return min(a, b); }); }
-template <int L>
 __device__ __forceinline__ float sum_over(float v) { return over_lanes<L>(v, [](float a, float b) { return a + b; }); }
 
 // exp(x), x <= 0, to 2 units of the last place: the exponent's rounding error is multiplied in
@@ -49,49 +48,49 @@ __device__ __forceinline__ float exp_near(float x)
     return x < -150.f ? 0.f : fmaf(e, lo * 0.69314718f, e);             // (also -infinity, whose lo is NaN)
 }
 
+// This lane's elements of a row of N (what is beyond it repeats its end): all loads without a branch between them, so that they are in flight together
+template <int L, int V, typename T>
+__device__ __forceinline__ void load_row(T (&v)[V], const T *row, int N, int lane)
+{
+    typedef __attribute__((__vector_size__(16))) T quad;
+    if (!(N & 3)) {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const quad a = *reinterpret_cast<const quad *>(row + min(4 * (i * L + lane), N - 4));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[4 * i + q] = a[q];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = row[min(4 * ((i / 4) * L + lane) + i % 4, N - 1)];
+    }
+}
+
 // The values of token t in this lane, -infinity where there is none
 template <int L, int V>
 __device__ __forceinline__ void load_values(float (&v)[V], const float *logits, const float *bias, int t, int N, int lane)
 {
-    const float *row = logits + (size_t)t * N;
+    load_row<L, V>(v, logits + (size_t)t * N, N, lane);
+    if (bias) {
+        float b[V];
+        load_row<L, V>(b, bias, N, lane);
 #pragma unroll
-    for (int i = 0; i < V / 4; ++i) {
-        const int col = 4 * (i * L + lane);
-        if (!(N & 3)) {
-            f32x4 a = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if (col < N) {
-                a = *reinterpret_cast<const f32x4 *>(row + col);
-                if (bias) {
-                    const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + col);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) a[q] = b[q] == -INFINITY ? -INFINITY : a[q] + b[q];
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) v[4 * i + q] = a[q];
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float a = -INFINITY;
-                if (col + q < N) {
-                    a = row[col + q];
-                    if (bias) a = bias[col + q] == -INFINITY ? -INFINITY : a + bias[col + q];
-                }
-                v[4 * i + q] = a;
-            }
-        }
+        for (int i = 0; i < V; ++i) v[i] = b[i] == -INFINITY ? -INFINITY : v[i] + b[i];
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (4 * ((i / 4) * L + lane) + i % 4 >= N) v[i] = -INFINITY;
 }
 
-// v -> e = exp(v - top); returns 1 / sum (0 for a token without an expert)
+// v -> e = exp(v - base), base the largest (0 if there is none); returns 1 / sum (0 for a token without an expert)
 template <int L, int V>
-__device__ __forceinline__ float exponentials(const float (&v)[V], float (&e)[V])
+__device__ __forceinline__ float exponentials(const float (&v)[V], float (&e)[V], float &base)
 {
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < V; ++i) top = fmaxf(top, v[i]);
     top = max_over<L>(top);
-    const float base = top == -INFINITY ? 0.f : top;
+    base = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) e[i] = exp_near(v[i] - base), sum += e[i];
@@ -99,10 +98,43 @@ __device__ __forceinline__ float exponentials(const float (&v)[V], float (&e)[V]
     return sum == 0.f ? 0.f : 1.f / sum;
 }
 
-template <int L, int V>
-__global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 3 : 1) void topk_kernel(TopkIo io, int per_block)
+// A value and its column as one double, ordered by the value and among equal ones from the highest column to the lowest: the value's bits are the upper word (three bits
+// of its fraction count as exponent, which keeps the order, and no finite or infinite value becomes a NaN), the column, or its complement under a positive value, the
+// lower.  One v_max_f64 compares both.  What cannot be chosen (-infinity, NaN, chosen before) is kGone, below all of them.
+constexpr uint32_t kGone = 0xffe00000u;
+__device__ __forceinline__ double ordered(float v, int col)
 {
-    constexpr int TPB = kThreads / L, MOST = L * V < 64 ? L * V : 64, KR = (MOST + L - 1) / L;
+    const uint32_t hi = __float_as_uint(v + 0.f);           // (-0 is 0)
+    const uint32_t lo = (int)hi < 0 ? (uint32_t)col : ~(uint32_t)col;
+    const bool none = !(v > -INFINITY);
+    return __hiloint2double((int)(none ? kGone : hi), (int)(none ? 0u : lo));
+}
+__device__ __forceinline__ double larger(double a, double b)
+{
+    double r;   // (fmax would quiet NaNs first, of which there are none)
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+template <int CTRL>
+__device__ __forceinline__ double larger_of(double v)
+{
+    return larger(v, __hiloint2double(dpp<CTRL>(__double2hiint(v)), dpp<CTRL>(__double2loint(v))));
+}
+template <int L>
+__device__ __forceinline__ double largest_over(double v)
+{
+    v = larger_of<0xB1>(v), v = larger_of<0x4E>(v);
+    if constexpr (L >= 8) v = larger_of<0x141>(v);
+    if constexpr (L >= 16) v = larger_of<0x140>(v);
+    if constexpr (L >= 32) v = larger(v, __shfl_xor(v, 16, 64));
+    if constexpr (L >= 64) v = larger(v, __shfl_xor(v, 32, 64));
+    return v;
+}
+
+template <int L, int V>
+__global__ __launch_bounds__(kThreads, V == 4 ? 8 : V == 8 ? 6 : V == 16 ? 4 : V == 32 ? 2 : 1) void topk_kernel(TopkIo io, int per_block)
+{
+    constexpr int TPB = kThreads / L;
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     const int first = blockIdx.x * per_block, last = min(io.T, first + per_block);
     float total[V];
@@ -112,52 +144,55 @@ __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 3 : 
         const int t = t0 + slot;
         const bool live = t < last;
         float v[V], e[V];
-        load_values<L, V>(v, io.logits, io.bias, min(t, last - 1), io.N, lane);
-        const float inv = exponentials<L, V>(v, e);
+        int own = lane;
+        const float *bias = io.bias;
+        asm volatile("" : "+v"(own), "+s"(bias));   // (what the loads need is not kept in registers from token to token)
+        load_values<L, V>(v, io.logits, bias, min(t, last - 1), io.N, own);
+        float base;
+        const float inv = exponentials<L, V>(v, e, base);
         if (io.partial || io.p_sum) {
             const float scale = live ? inv : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) total[i] = live ? fmaf(e[i], scale, total[i]) : total[i];
         }
-        // the choices: lane j % L keeps the j-th
-        int chosen[KR];
-        float mine[KR], sum = 0.f;
+        double key[V];
 #pragma unroll
-        for (int r = 0; r < KR; ++r) {
-            chosen[r] = -1, mine[r] = 0.f;
-            for (int jj = 0; jj < L; ++jj) {
-                if (r * L + jj >= io.k) break;
-                float best = v[0];
+        for (int i = 0; i < V; ++i) key[i] = ordered(v[i], 4 * ((i / 4) * L + lane) + i % 4);
+        // the choices, L at a time: lane j % L keeps the j-th.  Their weights are divided when all are known: those of earlier rounds lie in the output until then.
+        float sum = 0.f, mine = 0.f;
+        bool more = true;
+        int32_t *idx = io.idx + (size_t)t * io.k + lane;
+        float *weight = io.weight + (size_t)t * io.k + lane;
+        for (int j0 = 0; j0 < io.k; j0 += L) {
+            int chosen = -1;
+            mine = 0.f;
+            for (int jj = 0; more && jj < L && j0 + jj < io.k; ++jj) {
+                double top[V / 2];      // (pairs, then pairs of those: not one chain of V)
 #pragma unroll
-                for (int i = 1; i < V; ++i) best = fmaxf(best, v[i]);
-                best = max_over<L>(best);
-                int col = 1 << 30;
-                float ex = 0.f;
+                for (int i = 0; i < V / 2; ++i) top[i] = larger(key[2 * i], key[2 * i + 1]);
 #pragma unroll
-                for (int i = V - 1; i >= 0; --i)
-                    if (v[i] == best) col = 4 * (i / 4) * L + i % 4, ex = e[i];
-                const int at = min_over<L>(col == 1 << 30 ? col : col + 4 * lane);
-                if (best == -INFINITY || at == 1 << 30) break;          // (the second: nothing but NaN is left)
-                const int rel = at - 4 * lane;                          // the lane's value that goes
-                const bool here = col == rel;
+                for (int m = V / 4; m >= 1; m /= 2)
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (4 * (i / 4) * L + i % 4 == rel) v[i] = -INFINITY;
-                ex = sum_over<L>(here ? ex : 0.f);                      // one lane's value
+                    for (int i = 0; i < m; ++i) top[i] = larger(top[i], top[i + m]);
+                const double best = largest_over<L>(top[0]);
+                const int hi = __double2hiint(best), lo = __double2loint(best);
+                more = (uint32_t)hi != kGone;
+                if (!more) break;
+#pragma unroll
+                for (int i = 0; i < V; ++i) key[i] = key[i] == best ? __hiloint2double((int)kGone, lo) : key[i];
+                const float ex = exp_near(__int_as_float(hi) - base);
                 sum += ex;
-                if (lane == jj) chosen[r] = at, mine[r] = ex;
+                if (lane == jj) chosen = hi < 0 ? lo : ~lo, mine = ex;
+            }
+            if (live && j0 + lane < io.k) {
+                idx[j0] = chosen;
+                if (j0 + L < io.k) weight[j0] = mine;
             }
         }
         if (live) {
             const float scale = !io.normalize || inv != inv ? inv : sum == 0.f ? 0.f : 1.f / sum;   // (NaN stays)
-#pragma unroll
-            for (int r = 0; r < KR; ++r) {
-                const int j = r * L + lane;
-                if (j < io.k) {
-                    io.idx[(size_t)t * io.k + j] = chosen[r];
-                    io.weight[(size_t)t * io.k + j] = chosen[r] < 0 && inv == inv ? 0.f : mine[r] * scale;
-                }
-            }
+            for (int j0 = 0; j0 < io.k; j0 += L)
+                if (j0 + lane < io.k) weight[j0] = (j0 + L < io.k ? weight[j0] : mine) * scale;
         }
     }
     if (!io.partial && !io.p_sum) return;
@@ -199,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void topk_sum_kernel(const float *partial
 // dlogits = p (u - sum p u), + w (dweight - sum w dweight) at the chosen columns of normalised weights.  The chosen values are gathered through the
 // token's lanes: each lane compares the columns that it holds.
 template <int L, int V>
-__global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 3 : 1) void topk_backward_kernel(TopkGradIo io)
+__global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 2 : 1) void topk_backward_kernel(TopkGradIo io)
 {
     const int lane = threadIdx.x % L;
     const long long id = (long long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
@@ -207,25 +242,32 @@ __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 3 : 
     const int t = (int)id;
     float v[V], p[V], u[V];
     load_values<L, V>(v, io.logits, io.bias, t, io.N, lane);
-    const float inv = exponentials<L, V>(v, p);
+    float base;
+    const float inv = exponentials<L, V>(v, p, base);
+    int count[V];
+    if (io.count) load_row<L, V>(count, io.count, io.N, lane);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int col = 4 * ((i / 4) * L + lane) + i % 4;
         p[i] *= inv;
-        u[i] = 0.f;
-        if (io.count && col < io.N) u[i] = io.coef * (float)io.count[col];
+        u[i] = io.count ? io.coef * (float)count[i] : 0.f;
         v[i] = 0.f;                                                     // from here on: the gradient that reaches a chosen column
     }
     const size_t at = (size_t)t * io.k;
     std::conditional_t<(V > 32), uint64_t, uint32_t> picked = 0;        // of the lane's values
     constexpr decltype(picked) one = 1;
 #pragma unroll 1
-    for (int j = 0; j < io.k; ++j) {
-        const int col = io.idx[at + j], rel = col < io.N ? col - 4 * lane : -1;
-        const float dw = io.dweight[at + j];
+    for (int j0 = 0; j0 < io.k; j0 += 4) {                              // four choices' loads at a time
+        int col[4];
+        float dw[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += 4 * (i / 4) * L + i % 4 == rel ? dw : 0.f;
-        if (rel >= 0 && rel % (4 * L) < 4) picked |= one << (rel / (4 * L) * 4 + rel % 4);
+        for (int j = 0; j < 4; ++j) col[j] = j0 + j < io.k ? io.idx[at + j0 + j] : -1, dw[j] = j0 + j < io.k ? io.dweight[at + j0 + j] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int rel = (unsigned)col[j] < (unsigned)io.N ? col[j] - 4 * lane : -1;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += 4 * (i / 4) * L + i % 4 == rel ? dw[j] : 0.f;
+            if (rel >= 0 && rel % (4 * L) < 4) picked |= one << (rel / (4 * L) * 4 + rel % 4);
+        }
     }
     float of_chosen = 0.f, sum = 0.f, dot = 0.f;
     if (io.normalize) {
