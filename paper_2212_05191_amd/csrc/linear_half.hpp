@@ -118,13 +118,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
         constexpr int T = decltype(type)::value;
         constexpr bool IS_X = T == A0 || T == A1, TR = IS_X ? XT : WT;
         const char *base = IS_X ? xb : wb;
+        asm volatile("" : "+s"(base));   // scalar base + 32-bit offset, not a 64-bit sum for each lane
         lds_char *const to = lds + l_stage + kOff[T] + wave * 1024;
         if (decltype(whole)::value || l_left > 1 || l_last == 64) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint32_t o = off[2 * T + i];
-                asm volatile("" : "+v"(o));   // scalar base + 32-bit offset, not a 64-bit sum kept per lane
-                __builtin_amdgcn_global_load_lds(SMILE_GPTR(base + o), SMILE_LPTR(to + i * NW * 1024), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds(SMILE_GPTR(base + off[2 * T + i]), SMILE_LPTR(to + i * NW * 1024), 16, 0, 0);
             }
         } else {
 #pragma unroll
