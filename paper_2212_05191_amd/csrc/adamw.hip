@@ -135,6 +135,15 @@ struct AdamwStep {
     uint32_t seed;
 };
 
+// The moments' next values, every product and sum rounded by itself in the order that the formulas have: a state in 8 bits is rounded at random, and what decides it
+// should not depend on how a compiler contracts them.
+__device__ __forceinline__ void moments(const AdamwStep &a, float g, float &m, float &v)
+{
+#pragma clang fp contract(off)
+    m = a.beta1_f * m + a.rest1 * g;
+    v = a.beta2_f * v + a.rest2 * g * g;
+}
+
 template <int DT, int GDT, bool EIGHT, bool MASTER>
 __global__ __launch_bounds__(kThreads, kPerCu) void adamw_kernel(AdamwStep a)
 {
@@ -203,8 +212,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void adamw_kernel(AdamwStep a)
             const float decay = x.weight_decay;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                m[i] = fmaf(a.beta1_f, m[i], a.rest1 * g[i]);
-                v[i] = fmaf(a.beta2_f, v[i], a.rest2 * g[i] * g[i]);
+                moments(a, g[i], m[i], v[i]);
                 const float update = m[i] * inv1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inv2) + a.eps);
                 p[i] -= lr * fmaf(decay, p[i], update);
             }

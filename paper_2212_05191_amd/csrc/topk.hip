@@ -190,9 +190,11 @@ __global__ __launch_bounds__(kThreads, V == 4 ? 8 : V == 8 ? 6 : V == 16 ? 4 : V
             }
         }
         if (live) {
-            const float scale = !io.normalize || inv != inv ? inv : sum == 0.f ? 0.f : 1.f / sum;   // (NaN stays)
             for (int j0 = 0; j0 < io.k; j0 += L)
-                if (j0 + lane < io.k) weight[j0] = (j0 + L < io.k ? weight[j0] : mine) * scale;
+                if (j0 + lane < io.k) {
+                    const float ex = j0 + L < io.k ? weight[j0] : mine;
+                    weight[j0] = !io.normalize || inv != inv ? ex * inv : sum == 0.f ? 0.f : ex / sum;   // (NaN stays; a single choice has the weight 1)
+                }
         }
     }
     if (!io.partial && !io.p_sum) return;
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 2 : 
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         p[i] *= inv;
-        u[i] = io.count ? io.coef * (float)count[i] : 0.f;
+        u[i] = io.count ? io.coef * (float)(count[i] - io.count[0]) : 0.f;   // (a constant added to u changes nothing: even counts are told apart exactly)
         v[i] = 0.f;                                                     // from here on: the gradient that reaches a chosen column
     }
     const size_t at = (size_t)t * io.k;
@@ -269,14 +271,23 @@ __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 2 : 
             if (rel >= 0 && rel % (4 * L) < 4) picked |= one << (rel / (4 * L) * 4 + rel % 4);
         }
     }
+    // A weight as p / sum with its rounding mended, so that it is 1 where one is chosen: what the weights' gradient then leaves is exactly nothing, which its rounding, beside a
+    // small coef, would not be.
     float of_chosen = 0.f, sum = 0.f, dot = 0.f;
+    auto weight_of = [&](float p) {
+        const float w = p * of_chosen;
+        return fmaf(fmaf(-w, sum, p), of_chosen, w);
+    };
     if (io.normalize) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (picked >> i & 1) sum += p[i], dot = fmaf(p[i], v[i], dot);
-        sum = sum_over<L>(sum), dot = sum_over<L>(dot);
+            if (picked >> i & 1) sum += p[i];
+        sum = sum_over<L>(sum);
         of_chosen = sum == 0.f ? 0.f : 1.f / sum;
-        dot *= of_chosen;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (picked >> i & 1) dot = fmaf(weight_of(p[i]), v[i], dot);
+        dot = sum_over<L>(dot);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -294,7 +305,7 @@ __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 2 : 
         for (int q = 0; q < 4; ++q) {
             const int n = 4 * i + q;
             d[q] = p[n] * (u[n] - mean);
-            if (io.normalize && (picked >> n & 1)) d[q] = fmaf(p[n] * of_chosen, v[n] - dot, d[q]);
+            if (io.normalize && (picked >> n & 1)) d[q] = fmaf(weight_of(p[n]), v[n] - dot, d[q]);
         }
         float *to = io.dlogits + (size_t)t * io.N + col;
         if (!(io.N & 3)) {

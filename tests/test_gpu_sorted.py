@@ -145,6 +145,38 @@ def test_topk_backward_against_differences():
         assert abs(slope - float((d.double() * direction.double()).sum())) <= 1e-5 * size + 1e-6   # h^2 and the roundings of the difference
 
 
+@pytest.mark.parametrize("N,k", [(2, 1), (7, 1), (128, 1), (300, 1), (6, 6)])
+def test_normalised_weights_without_freedom_send_nothing_back(N, k):
+    """One choice has the weight 1 whatever the logits: exactly no gradient, and beside a small balance term that term's alone"""
+    g = gen(N)
+    logits, count = normal(g, 500, N, std=3.0), torch.randint(0, 50, (N,), generator=g, device=DEV, dtype=torch.int32)
+    idx, weight, _ = run_topk(logits, k, None, True)
+    if k == 1:
+        assert bool((weight == 1).all())
+    dweight = normal(g, 500, k) if k == 1 else torch.ones(500, k, device=DEV)
+    d = torch.full((500, N), math.nan, device=DEV)
+    B.smile_topk_backward(logits, idx, dweight, d, normalize=True)
+    assert bool((d == 0).all()) if k == 1 else float(d.abs().max()) <= 4 * N * R.E32
+    B.smile_topk_backward(logits, idx, dweight, d, normalize=True, count=count, coef=1e-6)
+    if k == 1:
+        p = torch.softmax(logits.double(), 1)
+        u = 1e-6 * count.double()
+        want, size = p * (u - (p * u).sum(1, keepdim=True)), p * (u + (p * u).sum(1, keepdim=True))
+        near(d, want, size * (N + 60) * R.E32, "balance term alone")
+
+
+def test_balance_term_of_nearly_even_counts():
+    """Counts that differ in their last places: what counts is their differences, which fp32 keeps only if they are taken before the sums"""
+    g = gen(8)
+    logits = normal(g, 300, 5, std=2.0)
+    count = torch.tensor([10000000, 10000003, 9999998, 10000001, 10000000], dtype=torch.int32, device=DEV)
+    idx, _, _ = run_topk(logits, 2, None, False)
+    d = torch.full((300, 5), math.nan, device=DEV)
+    B.smile_topk_backward(logits, idx, torch.zeros(300, 2, device=DEV), d, count=count, coef=1e-3)
+    p, u = torch.softmax(logits.double(), 1), 1e-3 * (count.double() - 1e7)
+    near(d, p * (u - (p * u).sum(1, keepdim=True)), p * (u.abs() + (p * u.abs()).sum(1, keepdim=True)) * 64 * R.E32, "dlogits")
+
+
 # ------------------------------------------------------------------ sort
 
 @pytest.mark.parametrize("T,k,N", [(1, 1, 1), (3, 2, 5), (16, 2, 64), (1000, 3, 7), (2048, 2, 4), (2049, 2, 255), (700, 8, 257), (5003, 2, 15), (900, 5, 1024),
