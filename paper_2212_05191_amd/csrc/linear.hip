@@ -136,8 +136,8 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
     GradPlan p{};
     const bool half = a.dtype != SMILE_DTYPE_F32;
     // an fp32 tile of 64 x 64 outputs takes about as long for a slab of 64 terms, four of them on a CU, as one of 128 x 128 in 16 bits
-    auto time = [&](int size, double tiles, double slabs) {
-        return half ? linear_half_time(size == 256 ? kHalf256 : kHalf128, tiles, slabs, false) : linear_half_time(kHalf128, tiles / 2, 1.5 * slabs, false);
+    auto time = [&](LinearKind kind, int size, double tiles, double slabs) {
+        return half ? linear_half_time(size == 256 ? kHalf256 : kHalf128, kind, tiles, slabs, false) : linear_half_time(kHalf128, kind, tiles / 2, 1.5 * slabs, false);
     };
     auto tiles_of = [](int n, int size) { return (n + size - 1) / size; };
     p.parts = a.N, p.tile = kHalf128;
@@ -149,7 +149,7 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
             if (!half && size == 256) break;
             for (int n = 1; n <= kMostParts && (n == 1 || (long long)a.N * n * 256 <= a.rows); ++n) {
                 const double per_group = std::ceil((double)a.rows / a.N / n / 64);
-                const double t = time(size, (double)a.N * n * tiles_of(a.F, size) * tiles_of(a.K, size), per_group) + parts_time(n, elements);
+                const double t = time(kLinearWeightGrad, size, (double)a.N * n * tiles_of(a.F, size) * tiles_of(a.K, size), per_group) + parts_time(n, elements);
                 if (t < best) best = t, cuts = n, p.tile = size == 256 ? kHalf256 : kHalf128;
             }
         }
@@ -162,10 +162,10 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
     if (a.dx) {
         const int size = half ? 128 : kF32Tile, slabs = tiles_of(a.F, 64);
         const double per = (double)a.rows / a.N, tiles = (a.N == 1 ? std::ceil(per / size) : std::min((double)a.rows, a.N * std::max(1.0, per / size + 0.5))) * tiles_of(a.K, size);
-        double best = time(size, tiles, slabs);
+        double best = time(kLinearRowGrad, size, tiles, slabs);
         int cuts = 1;
         for (int n = 2; n <= kMostParts && 4 * n <= slabs; ++n) {
-            const double t = time(size, tiles * n, tiles_of(slabs, n)) + parts_time(n, (double)a.rows * a.K);
+            const double t = time(kLinearRowGrad, size, tiles * n, tiles_of(slabs, n)) + parts_time(n, (double)a.rows * a.K);
             if (t < best) best = t, cuts = n;
         }
         if (cuts > 1) {

@@ -27,16 +27,16 @@ hipError_t launch_typed(const LinearGemm &g, int rows, const Tuning &tune, hipSt
 
 }  // namespace
 
-// Estimated times, us.  Measured with bfloat16 and GELU in a graph, this kernel and the tiles of 128 x 128: 1024 -> 4096, 1 row 3.7 / 15.8, 16 4.4 / 15.8, 32 5.5 / 15.9,
-// 64 7.6 / 15.8, 128 11.9 / 18.8, 256 21.1 / 18.9, 512 40 / 20; 4096 -> 1024, 16 rows 9.5 / 47.8, 64 20.3 / 47.7, 256 21.5 / 54.7, 512 38.5 / 55; 64 groups 1024 -> 4096, 16
-// rows in all 20.7 / 21.7, 128 87 / 88, 1024 223 / 103 (the weights' bytes 26, 103, 103).  Here a workgroup's time goes with its rows and terms, and the
-// workgroups share the CUs; there a slab costs 0.7 us as long as the tiles do not fill the chip.
+// Estimated times, us.  Measured with bfloat16 and GELU in a graph, this kernel and the tiles of 128 x 128: 1024 -> 4096, 1 row 3.8 / 13.7, 16 4.5 / 13.8, 32 5.5 / 14.0,
+// 64 7.5 / 13.9, 128 11.9 / 17.0, 256 21.4 / 17.2, 512 40 / 17.6; 4096 -> 1024, 16 rows 9.6 / 38, 64 20.2 / 38, 256 21.3 / 45, 512 38.5 / 45; 256 -> 256, 256 rows 4.0 / 9.7;
+// 64 groups 1024 -> 4096, 16 rows in all 21.3 / 21.8, 128 97 / 90, 1024 225 / 104 (the weights' bytes 26, 103, 103).  Here a workgroup's time goes with its rows and terms,
+// and the workgroups share the CUs; there a slab costs 0.6 us as long as the tiles do not fill the chip.
 bool linear_few_applies(const LinearGemm &g)
 {
     const int rows = few_rows(g), size = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     const double k = g.K / 1024.0, cost = size == 16 ? 1.6 : size == 32 ? 2.5 : 4.3;
     const double here = row_tiles(g, size) * ((g.Nout + 15) / 16) / kLinearCus, tiles = row_tiles(g, 128) * ((g.Nout + 127) / 128) / (1.5 * kLinearCus);
-    return 3.2 + cost * k * std::max(1.0, here) < 5.0 + 10.9 * k * std::max(1.0, tiles);
+    return 3.2 + cost * k * std::max(1.0, here) < 6.0 + 9.6 * k * std::max(1.0, tiles);
 }
 
 hipError_t launch_linear_few(int dtype, const LinearGemm &g, const Tuning &tune, hipStream_t s)

@@ -29,17 +29,22 @@ hipError_t launch_typed(const LinearGemm &g, LinearKind kind, HalfTile tile, con
 }  // namespace
 
 // 256 x 256 outputs alone on a CU move half of the bytes from L2 that 128 x 128 do, but the epilogue waits for nobody and nobody multiplies meanwhile, and there
-// are a quarter as many tiles to spread.  Time of `tiles` tiles of `slabs` slabs, us: rounds of the chip, each slabs x time of a slab + what a tile costs beside it; from
-// three rounds on workgroups are out of step and share the last one.  Its figures, and what they stand for (bfloat16; measured, 256 and 128, in brackets the model):
-//   forward, 16384 rows 4096 -> 1024: 143 / 155 (135 / 147); 64 groups of 512 rows, 1024 -> 4096: 391 / 398 (399 / 407), with GELU 470 / 435 (497 / 461)
-//   gradient of x, 16384 rows 4096 -> 1024: 171 / 200 (168 / 187); of the weights, 64 groups: 395 / 460 (380 / 441)
-//   4096 rows 1024 -> 1024 (64 and 256 tiles): 30 / 19 (43 / 19); 16 groups of 512 rows 768 -> 2304 with GELU: 66 / 50 (85 / 67)
-double linear_half_time(HalfTile tile, double tiles, double slabs, bool gelu)
+// are a quarter as many tiles to spread.  Time of `tiles` tiles of `slabs` slabs, us: rounds of the chip, each slabs x time of a slab (shorter while CUs are idle) + what a
+// tile costs beside it; from two rounds on workgroups are out of step and share the last one.  Measured, bfloat16, 256 and 128 (in brackets the model):
+//   forward, 16384 rows 1024 -> 4096: 141 / 165 (143 / 170), with GELU 167 / 181 (170 / 189); 256 -> 4096: 71 / 67 (67 / 69), 98 / 87 (94 / 88)
+//   64 groups of 512 rows, 1024 -> 4096: 389 / 439 (349 / 376), GELU 418 / 440 (416 / 419); 16 groups of 512 rows, 768 -> 2304: 56 / 50 (61 / 51)
+//   gradient of x, 4096 rows, 4096 terms, 4096 columns: 116 / 137 (115 / 146), 1024 rows and columns in 32 / 64 tiles: 73 / 45 (77 / 47)
+//   gradient of the weights, 16384 x 4096 of 1024 rows: 129 / 154 (130 / 163); 2048 x 1024 of 4096 rows: 72 / 43 (74 / 46)
+double linear_half_time(HalfTile tile, LinearKind kind, double tiles, double slabs, bool gelu)
 {
-    auto shared = [](double n) { return n <= 3.0 ? std::ceil(n) : n + 0.25; };
-    if (tile == kHalf256) return 5.0 + shared(tiles / kLinearCus) * (1.9 * slabs + (gelu ? 17.5 : 8.0));
-    const double n = tiles / (2 * kLinearCus), beside = gelu ? 8.0 : 5.0;
-    return 5.0 + (n <= 0.5 ? 0.68 * slabs + 0.6 * beside : shared(n) * (1.06 * slabs + beside));
+    auto shared = [](double n) { return n <= 2.0 ? std::ceil(n) : std::min(std::ceil(n), n + 0.25); };
+    const double n = tiles / (tile == kHalf256 ? kLinearCus : 2 * kLinearCus), full = std::min(n, 1.0);
+    if (tile == kHalf256) {
+        const double beside = kind == kLinearWeightGrad ? 6.0 : kind == kLinearRowGrad ? 8.5 : gelu ? 16.0 : 9.3;
+        return 5.0 + shared(n) * ((0.95 + 0.62 * full * full) * slabs + beside);
+    }
+    const double beside = kind == kLinearWeightGrad ? 3.0 : kind == kLinearRowGrad ? 3.5 : gelu ? 6.2 : 3.8;
+    return 5.0 + shared(n) * ((0.59 + 0.46 * full * full) * slabs + (n <= 1.0 ? 0.5 : 1.0) * beside);
 }
 
 // Groups of unknown rows are taken as even, with half a tile more each
@@ -48,9 +53,9 @@ HalfTile pick_half_tile(LinearKind kind, const LinearGemm &g)
     auto time = [&](HalfTile tile) {
         const int size = tile == kHalf256 ? 256 : 128;
         const double cols = (g.Nout + size - 1) / size, per = (double)g.rows / g.N;
-        if (kind == kLinearWeightGrad) return linear_half_time(tile, (double)g.parts * ((g.Mrows + size - 1) / size) * cols, std::ceil((double)g.rows / g.parts / 64), false);
+        if (kind == kLinearWeightGrad) return linear_half_time(tile, kind, (double)g.parts * ((g.Mrows + size - 1) / size) * cols, std::ceil((double)g.rows / g.parts / 64), false);
         const double tiles = g.N == 1 ? std::ceil(per / size) : std::min((double)g.rows, g.N * std::max(1.0, per / size + 0.5));
-        return linear_half_time(tile, g.parts * tiles * cols, std::ceil((double)g.K / g.parts / 64), g.act == 2);
+        return linear_half_time(tile, kind, g.parts * tiles * cols, std::ceil((double)g.K / g.parts / 64), g.act == 2);
     };
     return time(kHalf256) <= time(kHalf128) ? kHalf256 : kHalf128;
 }

@@ -2,15 +2,16 @@
 //
 // A workgroup of WM x WN waves computes BM x BN outputs at a time, a wave (64 QA) x 64 of them, and walks the tiles of the launch.  A slab (64 terms) is four
 // units: the rows of X of the first and of the second half of every wave's blocks (A0, A1), and the same of W (B0, B1).  It is multiplied in two phases: A0 with B0
-// and B1, then A1; a phase reads what it does not hold yet from LDS and multiplies.  LDS holds two slabs; a unit's slot is refilled
-// one phase after its reading, two slabs ahead, so that four to five of the eight units are in flight at any time (with four phases of one product five to seven are, but
-// twice the barriers cost more: 8192^3 1017 -> 971 us).  The stream of slabs runs on through the
-// tiles: the epilogue finds the next tile's first two slabs requested.  Behind the last tile the last slab is requested again, so that every wait
-// counts the same.
+// and B1, then A1; a phase reads what it does not hold yet from LDS, then multiplies.  LDS holds two slabs; a unit's slot is refilled one phase after its reading, two
+// slabs ahead, so that four to five of the eight units are in flight at any time.  Four phases of one product each, twice the barriers, were slower (8192^3 1017 against
+// 971 us when both were tried); so was reading between the products of the phase before, with the fragments of two phases in registers (128 x 128 tiles, 4096 rows 1024
+// -> 1024: 19.0 against 17.5 us).  The stream of slabs runs on through the tiles: the epilogue finds the next tile's first two slabs requested.  Behind the last tile the
+// last slab is requested again, so that every wait counts the same.
 //
 // What bounds it: the matrix cores, if what they are fed with keeps up.  A wave that reads its fragments (up to 16 of 16 bytes a lane) cannot multiply, so two waves
 // of a SIMD take turns (STAGGER): the waves are two halves, one a barrier behind the other; while one multiplies the other reads and requests.  With
-// four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.
+// four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.  On a full chip a slab of 256 x 256 takes 1.56 us (1380
+// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1080); an epilogue about 9 and 4 us, 16 and 6 with GELU.  8192^3: 797 us (1380 TFLOP/s).
 //
 // Operand units in LDS.  Normal: [row][64 k], piece c (16 bytes) of a row at c ^ ((row >> 1) & 7).  Transposed: as in memory, [64 k][columns], fragments by
 // transposing reads; pieces rotated by 4 (k & 3) in rows of 16 pieces, by 4 ((k >> 1) & 1) in rows of 8, so that successive k-rows fall on distinct banks.

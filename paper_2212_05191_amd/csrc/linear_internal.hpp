@@ -29,7 +29,7 @@ enum HalfTile { kHalf256, kHalf128 };
 // what the choice of a tile and the cuts of the gradients' sums go by: their workspace is asked for on the host alone
 constexpr int kLinearCus = 256;
 HalfTile pick_half_tile(LinearKind kind, const LinearGemm &g);
-double linear_half_time(HalfTile tile, double tiles, double slabs, bool gelu);   // estimated, us
+double linear_half_time(HalfTile tile, LinearKind kind, double tiles, double slabs, bool gelu);   // estimated, us
 hipError_t launch_linear_half(int dtype, const LinearGemm &g, LinearKind kind, HalfTile tile, const Tuning &tune, hipStream_t s);
 
 // The forward product of few rows (linear_few.hip), and whether it is the faster one
