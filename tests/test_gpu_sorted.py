@@ -381,6 +381,35 @@ def test_linear_of_a_skewed_router(dtype):
     run_linear_backward(g, x, w, kept, "gelu", start, live, dtype)
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f16"))
+@pytest.mark.parametrize("name,N,rows,K,F,behind,skew", [("gelu", 1, 7900, 712, 2040, 0, False), ("relu", 1, 8190, 776, 2040, 5, False), ("gelu", 5, 7000, 2040, 1288, 100, False),
+                                                         ("none", 9, 15500, 2056, 1544, 33, True)])
+def test_linear_of_many_rows(name, N, rows, K, F, behind, skew, dtype):
+    """Enough tiles of 256 x 256 for the chip: terms, rows and columns that end inside them, rows of no group, groups of a few rows and of most"""
+    g = gen(rows)
+    start = starts(g, N, rows, behind, skew=skew)
+    x, w, b, res, y, kept, live = run_linear(g, N, rows, K, F, dtype, name, True, True, start, pre=True, poison=True)
+    run_linear_backward(g, x, w, kept if name != "none" else None, name, start, live, dtype)
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f16"))
+def test_weights_gradient_of_many_rows_in_parts(dtype):
+    """16000 rows in two parts of 256 x 256 tiles, their sums joined"""
+    g = gen(17)
+    rows, K, F = 16000, 2800, 2800
+    start = torch.tensor([0, rows - 77], dtype=torch.int32, device=DEV)
+    dy, x, dw = normal(g, rows, F, dtype=dtype), normal(g, rows, K, dtype=dtype), torch.full((1, F, K), math.nan, dtype=TYPES[dtype], device=DEV)
+    dy[rows - 77:], x[rows - 77:] = math.nan, math.nan
+    args = B.make_linear_backward_args(dy, x, dw, dw=dw, start=start)
+    nbytes = B.smile_linear_backward_workspace_bytes(args)
+    assert nbytes >= 2 * F * K * 4
+    B.smile_linear_backward(args, scratch(nbytes).fill_(0xFF))
+    a, b = dy[:rows - 77].double(), x[:rows - 77].double()
+    want = a.T.contiguous() @ b
+    tol = a.abs().T.contiguous() @ b.abs() * (rows + 2) * R.E32
+    near(dw[0], want, tol * (1 + R.HALF[TYPES[dtype]]) + R.half_step(want, TYPES[dtype]) * (1 + 1e-3), "dw")
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_linear_without_any_row(dtype):
     """First rows that are all the same: nothing is written but zeros of the weights' gradients; and one group that holds everything."""
@@ -404,7 +433,7 @@ def test_linear_with_first_rows_out_of_order_stays_in_its_tensors():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,K,F", [(16, 256, 136), (300, 200, 264), (700, 512, 520)])
+@pytest.mark.parametrize("rows,K,F", [(16, 256, 136), (300, 200, 264), (700, 512, 520), (7900, 712, 2040)])
 def test_linear_keeps_nan_and_infinity_in_their_row_and_column(rows, K, F, dtype):
     g = gen(9)
     x, w = normal(g, rows, K, dtype=dtype), normal(g, 1, F, K, std=0.1, dtype=dtype)
@@ -588,6 +617,50 @@ def test_unpacked_states(dtype):
 
 
 # ------------------------------------------------------------------ streams and graphs
+
+def test_operators_run_on_the_stream_that_is_current():
+    """Work behind a long run of another stream is neither waited for nor disturbed; the stream's own order holds"""
+    g = gen(31)
+    x, w = normal(g, 2000, 512, dtype="bf16"), normal(g, 1, 1024, 512, std=0.05, dtype="bf16")
+    logits = normal(g, 2000, 16)
+    want, want_idx = torch.zeros(2000, 1024, dtype=torch.bfloat16, device=DEV), R.topk(logits, None, 2, True)[0]
+    B.smile_linear(B.make_linear_args(x, w, want, act="relu"))
+    late, late_logits, y = torch.zeros_like(x), torch.zeros_like(logits), torch.zeros_like(want)
+    big = normal(g, 4096, 4096)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        for _ in range(20):
+            big = (big @ big).clamp(-1, 1)
+        late.copy_(x)
+        late_logits.copy_(logits)
+        B.smile_linear(B.make_linear_args(late, w, y, act="relu"))
+        idx, weight, _ = run_topk(late_logits, 2, None, True, p_sum=False)
+    stream.synchronize()
+    assert torch.equal(y, want) and torch.equal(idx, want_idx)
+    y.zero_()
+    torch.cuda.synchronize()
+    B.smile_linear(B.make_linear_args(x, w, y, act="relu"), stream=stream)
+    stream.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_tensors_of_the_host_are_refused():
+    z = torch.zeros
+    with pytest.raises(ValueError):
+        B.smile_topk(z(4, 8), ints(4, 2), z(4, 2, device=DEV))
+    with pytest.raises(ValueError):
+        B.smile_sorted_dispatch(z(4, 64, device=DEV), ints(4, 2), z(8, 64))
+    x, w, y = z(4, 64, device=DEV), z(1, 72, 64), z(4, 72, device=DEV)
+    with pytest.raises(ValueError):
+        B.smile_linear(B.make_linear_args(x, w, y))
+    args = B.make_linear_backward_args(y, x, w.to(DEV), dbias=z(72, device=DEV))
+    with pytest.raises(ValueError):
+        B.smile_linear_backward(args, torch.zeros(B.smile_linear_backward_workspace_bytes(args), dtype=torch.uint8))
+    opt = B.AdamW([dict(param=z(8, device=DEV), grad=z(8, device=DEV), m=z(8, device=DEV), v=z(8, device=DEV))])
+    with pytest.raises(ValueError):
+        B.smile_adamw(opt, z(1), ints(1))
+
 
 def test_captured_step_follows_its_inputs():
     """A training step of the operators, captured once and replayed with other inputs, a new learning rate and the step's own count, beside eager work"""
