@@ -494,6 +494,7 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
  * products of each expert's rows (or of dense rows), the weighted return, the gradients, and an AdamW step.  They need no ctx and
  * allocate nothing.  Workspaces are the caller's, 256-byte aligned, and only used during the call's enqueued work; calls that overlap must not share
  * one.  The functions ending in _bytes, and smile_adamw_plan, work on the host alone.
+ * What a call writes must not overlap what it reads or writes besides, but where a tensor may be another: SMILE_INVALID_ARG.
  * Limits: T, rows, N, k, d, K, F >= 1; N <= 4096; k <= N and k <= 64; T*k < 2^26, rows and R <= 2^27; d, K, F % 8 == 0; d <= 16384,
  * K, F <= 32768; elements of any tensor below 2^40.
  * Indices and row numbers are never followed outside their tensors: a pair whose expert is not in 0 .. N - 1 has no row, a row number that is not in
@@ -517,7 +518,7 @@ smile_status smile_topk(int32_t T, int32_t N, int32_t k, int32_t normalize, cons
  *   normalize:      the same without dweight, and + w (dweight[t,j] - sum_j w dweight[t,:]) at e = idx[t,j], w the weights
  * idx as smile_topk gave it (a token's experts differ).  coef = alpha * N / (k T^2) makes the second term
  * alpha N sum_e f_e P_e, Eq. 4 of one level with the fractions f_e = count[e] / (k T) and P_e = p_sum[e] / T.
- * dlogits[T,N] fp32; the sum of it over t is the gradient of the bias. */
+ * dlogits[T,N] fp32, may be logits; the sum of it over t is the gradient of the bias. */
 smile_status smile_topk_backward(int32_t T, int32_t N, int32_t k, int32_t normalize, const float *logits, const float *bias, const int32_t *idx,
                                  const float *dweight, const int32_t *count, float coef, float *dlogits, void *stream);
 
@@ -529,7 +530,8 @@ smile_status smile_sort_experts_workspace_bytes(int32_t T, int32_t k, int32_t N,
 smile_status smile_sort_experts(int32_t T, int32_t k, int32_t N, const int32_t *idx, int32_t *count, int32_t *start, int32_t *pos, int32_t *source,
                                 void *workspace, size_t workspace_bytes, void *stream);
 
-/* Tokens to their sorted rows: xs[pos[t,j],:] = x[t,:].  x[T,d], xs[R,d] in `dtype`; rows no pair has are left as they were. */
+/* Tokens to their sorted rows: xs[pos[t,j],:] = x[t,:].  x[T,d], xs[R,d] in `dtype`; rows no pair has are left as they were, and no row may have
+ * two pairs (here and in smile_sorted_combine_backward: either's could remain). */
 smile_status smile_sorted_dispatch(int32_t T, int32_t k, int32_t d, int32_t R, int32_t dtype, const void *x, const int32_t *pos, void *xs, void *stream);
 
 /* And back: y[t,:] = residual[t,:] + sum_j weight[t,j] * ys[pos[t,j],:], in fp32, rounded once.  weight NULL: ones, which makes it the gradient of
@@ -538,7 +540,7 @@ smile_status smile_sorted_combine(int32_t T, int32_t k, int32_t d, int32_t R, in
                                   const void *residual, void *y, void *stream);
 
 /* Its gradients: dys[pos[t,j],:] = weight[t,j] * dy[t,:], dweight[t,j] = sum_c dy[t,c] * ys[pos[t,j],c] (fp32; 0 for a pair without a row).
- * Rows of dys no pair has are left as they were.  dys must not overlap dy or ys.  dweight and ys may be NULL together. */
+ * Rows of dys no pair has are left as they were.  dweight and ys may be NULL together. */
 smile_status smile_sorted_combine_backward(int32_t T, int32_t k, int32_t d, int32_t R, int32_t dtype, const void *dy, const void *ys, const int32_t *pos,
                                            const float *weight, void *dys, float *dweight, void *stream);
 
@@ -590,7 +592,7 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
  * its parameter and first moment NaN, its v the largest code, and does not count for the block's power of two.
  * A state that decayed below fp32's normal range is kept as far as the codes reach.
  * The tensors of a plan share their types; each pointer is 16-byte aligned, the scales' excepted.  The plan is built on the host and copied to the device by the
- * caller (the device copy 256-byte aligned; the step keeps a counter in it, so steps of one plan must not overlap). */
+ * caller (no tensor or state twice in it; the device copy 256-byte aligned; the step keeps a counter in it, so steps of one plan must not overlap). */
 typedef struct smile_adamw_tensor {
     void *param;                 /* [n] in `dtype` */
     const void *grad;            /* [n] in `grad_dtype` */

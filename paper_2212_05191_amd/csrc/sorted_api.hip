@@ -3,6 +3,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
+#include <memory>
+#include <new>
 
 #include "api_checks.hpp"
 #include "sorted_internal.hpp"
@@ -21,6 +24,29 @@ bool bad_workspace(const void *p, size_t bytes, size_t needed)
 {
     return needed != 0 && ((reinterpret_cast<uintptr_t>(p) & 255u) != 0 || bytes < needed);
 }
+
+// memory of a call: NULL overlaps nothing
+struct Span {
+    const void *at;
+    size_t bytes;
+};
+bool overlap(Span a, Span b)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
+    return p && q && p < q + b.bytes && q < p + a.bytes;
+}
+// one of what is written overlaps another, or what is read (`same`: but for the first one written, which may be exactly that)
+bool overlapping(std::initializer_list<Span> written, std::initializer_list<Span> read, const void *same = nullptr)
+{
+    for (auto w = written.begin(); w != written.end(); ++w) {
+        for (auto o = w + 1; o != written.end(); ++o)
+            if (overlap(*w, *o)) return true;
+        for (const Span &r : read)
+            if (overlap(*w, r) && !(w == written.begin() && same && w->at == same && r.at == same)) return true;
+    }
+    return false;
+}
+Span words(const void *at, double n) { return {at, (size_t)n * 4}; }
 
 smile_status check_choices(int T, int N, int k)
 {
@@ -79,6 +105,24 @@ smile_status check_adamw_tensors(const smile_adamw_args &a, const smile_adamw_te
     return SMILE_OK;
 }
 
+// What a step writes, tensor by tensor: nothing of it may be there twice, or its steps would race
+smile_status check_adamw_apart(const smile_adamw_args &a, const smile_adamw_tensor *tensors)
+{
+    const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)a.tensors * 6]);
+    if (!spans) return SMILE_HIP_ERROR;
+    Span *end = spans.get();
+    for (int i = 0; i < a.tensors; ++i) {
+        const smile_adamw_tensor &x = tensors[i];
+        const size_t n = (size_t)x.n, blocks = (n + 127) / 128, state = a.state_bits == 8 ? blocks * 128 : n * 4;
+        for (const Span &w : {Span{x.param, n * elem_size(a.dtype)}, Span{x.master, n * 4}, Span{x.m, state}, Span{x.v, state}, Span{x.m_scale, blocks}, Span{x.v_scale, blocks}})
+            if (w.at) *end++ = w;
+    }
+    std::sort(spans.get(), end, [](const Span &p, const Span &q) { return p.at < q.at; });
+    for (const Span *w = spans.get(); w + 1 < end; ++w)
+        if (overlap(w[0], w[1])) return SMILE_INVALID_ARG;
+    return SMILE_OK;
+}
+
 size_t adamw_plan_bytes(int tensors, long long chunks) { return kAdamwTensorsAt + (size_t)tensors * sizeof(AdamwTensor) + (size_t)chunks * sizeof(AdamwChunk); }
 
 }  // namespace
@@ -107,6 +151,8 @@ smile_status smile_topk(int32_t T, int32_t N, int32_t k, int32_t normalize, cons
     const size_t needed = p_sum ? topk_workspace(T, N) : 0;
     if (needed && !workspace) return SMILE_INVALID_ARG;
     if (bad_workspace(workspace, workspace_bytes, needed)) return SMILE_WORKSPACE;
+    const double pairs = (double)T * k;
+    if (overlapping({words(idx, pairs), words(weight, pairs), words(p_sum, N)}, {words(logits, (double)T * N), words(bias, N)})) return SMILE_INVALID_ARG;
     return from_hip(launch_topk(TopkIo{logits, bias, idx, weight, p_sum, static_cast<float *>(workspace), T, N, k, normalize != 0},
                                 static_cast<hipStream_t>(stream)));
 }
@@ -117,6 +163,8 @@ smile_status smile_topk_backward(int32_t T, int32_t N, int32_t k, int32_t normal
     if (bad(logits) || bad_opt(bias) || bad(idx) || bad(dweight) || bad_opt(count) || bad(dlogits)) return SMILE_INVALID_ARG;
     const smile_status st = check_choices(T, N, k);
     if (st != SMILE_OK) return st;
+    const double all = (double)T * N, pairs = (double)T * k;
+    if (overlapping({words(dlogits, all)}, {words(logits, all), words(bias, N), words(idx, pairs), words(dweight, pairs), words(count, N)}, logits)) return SMILE_INVALID_ARG;
     return from_hip(launch_topk_backward(TopkGradIo{logits, bias, idx, dweight, count, coef, dlogits, T, N, k, normalize != 0},
                                          static_cast<hipStream_t>(stream)));
 }
@@ -138,6 +186,8 @@ smile_status smile_sort_experts(int32_t T, int32_t k, int32_t N, const int32_t *
     if (st != SMILE_OK) return st;
     if (needed && !workspace) return SMILE_INVALID_ARG;
     if (bad_workspace(workspace, workspace_bytes, needed)) return SMILE_WORKSPACE;
+    const double pairs = (double)T * k;
+    if (overlapping({words(count, N), words(start, N + 1.0), words(pos, pairs), words(source, pairs)}, {words(idx, pairs)})) return SMILE_INVALID_ARG;
     return from_hip(launch_sort_experts(SortIo{idx, count, start, pos, source, static_cast<int32_t *>(workspace), T * k, N}, static_cast<hipStream_t>(stream)));
 }
 
@@ -146,6 +196,8 @@ smile_status smile_sorted_dispatch(int32_t T, int32_t k, int32_t d, int32_t R, i
     if (bad(x) || bad(pos) || bad(xs)) return SMILE_INVALID_ARG;
     const smile_status st = check_rows(T, k, d, R, dtype);
     if (st != SMILE_OK) return st;
+    const size_t row = (size_t)d * elem_size(dtype), pairs = (size_t)T * k;
+    if (overlapping({{xs, R * row}}, {{x, T * row}, words(pos, pairs)})) return SMILE_INVALID_ARG;
     return from_hip(launch_sorted_dispatch(dtype, SortedRowsIo{x, nullptr, pos, nullptr, nullptr, xs, nullptr, T, k, d, R}, static_cast<hipStream_t>(stream)));
 }
 
@@ -155,6 +207,8 @@ smile_status smile_sorted_combine(int32_t T, int32_t k, int32_t d, int32_t R, in
     if (bad(ys) || bad(pos) || bad_opt(weight) || bad_opt(residual) || bad(y)) return SMILE_INVALID_ARG;
     const smile_status st = check_rows(T, k, d, R, dtype);
     if (st != SMILE_OK) return st;
+    const size_t row = (size_t)d * elem_size(dtype), pairs = (size_t)T * k;
+    if (overlapping({{y, T * row}}, {{residual, T * row}, {ys, R * row}, words(pos, pairs), words(weight, pairs)}, residual)) return SMILE_INVALID_ARG;
     return from_hip(launch_sorted_combine(dtype, SortedRowsIo{ys, nullptr, pos, weight, residual, y, nullptr, T, k, d, R}, static_cast<hipStream_t>(stream)));
 }
 
@@ -162,9 +216,10 @@ smile_status smile_sorted_combine_backward(int32_t T, int32_t k, int32_t d, int3
                                            const float *weight, void *dys, float *dweight, void *stream)
 {
     if (bad(dy) || bad_opt(ys) || bad(pos) || bad(weight) || bad(dys) || bad_opt(dweight) || (ys == nullptr) != (dweight == nullptr)) return SMILE_INVALID_ARG;
-    if (dys == dy || dys == ys) return SMILE_INVALID_ARG;
     const smile_status st = check_rows(T, k, d, R, dtype);
     if (st != SMILE_OK) return st;
+    const size_t row = (size_t)d * elem_size(dtype), pairs = (size_t)T * k;
+    if (overlapping({{dys, R * row}, words(dweight, pairs)}, {{dy, T * row}, {ys, R * row}, words(pos, pairs), words(weight, pairs)})) return SMILE_INVALID_ARG;
     return from_hip(launch_sorted_combine_backward(dtype, SortedRowsIo{dy, ys, pos, weight, nullptr, dys, dweight, T, k, d, R}, static_cast<hipStream_t>(stream)));
 }
 
@@ -173,9 +228,11 @@ smile_status smile_linear(const smile_linear_args *p, void *stream)
     if (!p) return SMILE_INVALID_ARG;
     const smile_linear_args &a = *p;
     if (bad(a.x) || bad(a.w) || bad_opt(a.bias) || bad_opt(a.residual) || bad_opt(a.start) || bad(a.y) || bad_opt(a.pre)) return SMILE_INVALID_ARG;
-    if (a.y == a.x || a.pre == a.y || (a.pre && (a.pre == a.x || a.pre == a.residual))) return SMILE_INVALID_ARG;
     const smile_status st = check_linear(a.N, a.rows, a.K, a.F, a.dtype, a.act, a.start);
     if (st != SMILE_OK) return st;
+    const size_t es = elem_size(a.dtype), out = (size_t)a.rows * a.F * es, bias = (size_t)a.N * a.F * es;
+    if (overlapping({{a.y, out}, {a.pre, out}}, {{a.residual, out}, {a.x, (size_t)a.rows * a.K * es}, {a.w, bias * a.K}, {a.bias, bias}, words(a.start, a.N + 1.0)}, a.residual))
+        return SMILE_INVALID_ARG;
     return from_hip(launch_linear(a, device_tuning(), static_cast<hipStream_t>(stream)));
 }
 
@@ -195,6 +252,11 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
     const size_t needed = linear_backward_workspace(*args);
     if (needed && !workspace) return SMILE_INVALID_ARG;
     if (bad_workspace(workspace, workspace_bytes, needed)) return SMILE_WORKSPACE;
+    const smile_linear_backward_args &a = *args;
+    const size_t es = elem_size(a.dtype), in = (size_t)a.rows * a.K * es, out = (size_t)a.rows * a.F * es, bias = (size_t)a.N * a.F * es;
+    if (overlapping({{a.dx, in}, {a.dw, bias * a.K}, {a.dbias, bias}},
+                    {{a.dy, out}, {a.dw ? a.x : nullptr, in}, {a.dx ? a.w : nullptr, bias * a.K}, {a.act != SMILE_ACT_NONE ? a.pre : nullptr, out}, words(a.start, a.N + 1.0)}))
+        return SMILE_INVALID_ARG;
     return from_hip(launch_linear_backward(*args, device_tuning(), workspace, static_cast<hipStream_t>(stream)));
 }
 
@@ -214,6 +276,7 @@ smile_status smile_adamw_plan(smile_adamw_args *args, const smile_adamw_tensor *
     long long chunks = 0;
     smile_status st = check_adamw(*args);
     if (st == SMILE_OK) st = check_adamw_tensors(*args, tensors, chunks);
+    if (st == SMILE_OK) st = check_adamw_apart(*args, tensors);
     if (st != SMILE_OK) return st;
     if (plan_bytes < adamw_plan_bytes(args->tensors, chunks)) return SMILE_WORKSPACE;
     char *base = static_cast<char *>(plan);

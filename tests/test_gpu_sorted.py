@@ -145,6 +145,17 @@ def test_topk_backward_against_differences():
         assert abs(slope - float((d.double() * direction.double()).sum())) <= 1e-5 * size + 1e-6   # h^2 and the roundings of the difference
 
 
+@pytest.mark.parametrize("N", (5, 16, 300, 2051))
+def test_topk_backward_in_place(N):
+    g = gen(N)
+    logits, dweight = normal(g, 70, N), normal(g, 70, 2)
+    idx, _, _ = run_topk(logits, 2, None, True, p_sum=False)
+    want = torch.zeros_like(logits)
+    B.smile_topk_backward(logits, idx, dweight, want, normalize=True)
+    B.smile_topk_backward(logits, idx, dweight, logits, normalize=True)
+    assert torch.equal(logits, want)
+
+
 @pytest.mark.parametrize("N,k", [(2, 1), (7, 1), (128, 1), (300, 1), (6, 6)])
 def test_normalised_weights_without_freedom_send_nothing_back(N, k):
     """One choice has the weight 1 whatever the logits: exactly no gradient, and beside a small balance term that term's alone"""

@@ -159,6 +159,55 @@ def test_adamw_refusals():
     assert unpack(n=100) == B.BAD_SHAPE and unpack(n=0) == B.BAD_SHAPE and unpack(dtype=2) == B.UNSUPPORTED
 
 
+def test_overlapping_memory_is_refused():
+    """What is written lies apart from what is read and from what else is written, but where a tensor may be another.  (No call here gets as far as a launch: the first
+    rows that may coincide are covered on the GPU.)"""
+    lib = B.load()
+    M = 1 << 20                                             # pointers this far apart do not overlap
+    T, k, N, d, rows, F = 16, 2, 8, 64, 32, 128
+    topk = lambda **kw: lib.smile_topk(T, N, k, 1, *({**dict(logits=M, bias=2 * M, idx=3 * M, weight=4 * M, p_sum=5 * M), **kw}).values(), 6 * M, BIG, None)       # noqa: E731
+    for wrong in (dict(idx=M), dict(weight=M + 16), dict(p_sum=2 * M), dict(weight=3 * M + 64), dict(idx=M + T * N * 4 - 16)):
+        assert topk(**wrong) == B.INVALID_ARG, wrong
+    tback = lambda **kw: lib.smile_topk_backward(T, N, k, 1, *({**dict(logits=M, bias=2 * M, idx=3 * M, dweight=4 * M, count=5 * M), **kw}).values(), 1.0, 6 * M, None)     # noqa: E731
+    for wrong in (dict(logits=6 * M + 16), dict(bias=6 * M), dict(idx=6 * M + 64), dict(dweight=6 * M), dict(count=6 * M)):
+        assert tback(**wrong) == B.INVALID_ARG, wrong
+    sort = lambda **kw: lib.smile_sort_experts(T, k, N, *({**dict(idx=M, count=2 * M, start=3 * M, pos=4 * M, source=5 * M), **kw}).values(), 6 * M, BIG, None)      # noqa: E731
+    for wrong in (dict(pos=M), dict(source=4 * M), dict(count=3 * M + 32), dict(start=M + 64)):
+        assert sort(**wrong) == B.INVALID_ARG, wrong
+    assert lib.smile_sorted_dispatch(T, k, d, rows, 1, M, 2 * M, M + 16, None) == B.INVALID_ARG
+    assert lib.smile_sorted_dispatch(T, k, d, rows, 1, M, 2 * M, 2 * M + 16, None) == B.INVALID_ARG
+    combine = lambda **kw: lib.smile_sorted_combine(T, k, d, rows, 1, *({**dict(ys=M, pos=2 * M, weight=3 * M, residual=4 * M, y=5 * M), **kw}).values(), None)      # noqa: E731
+    for wrong in (dict(ys=5 * M), dict(pos=5 * M), dict(weight=5 * M + 16), dict(residual=5 * M + 16)):
+        assert combine(**wrong) == B.INVALID_ARG, wrong
+    back = lambda **kw: lib.smile_sorted_combine_backward(T, k, d, rows, 1, *({**dict(dy=M, ys=2 * M, pos=3 * M, weight=4 * M, dys=5 * M, dweight=6 * M), **kw}).values(), None)      # noqa: E731
+    for wrong in (dict(dys=M), dict(dys=2 * M + 128), dict(dweight=4 * M), dict(dweight=5 * M), dict(pos=6 * M)):
+        assert back(**wrong) == B.INVALID_ARG, wrong
+
+    def linear(cls, function, tail, **kw):
+        a = cls(N, rows, d, F, 1, kw.pop("act", 1))
+        for i, (name, _) in enumerate(cls._fields_[6:]):
+            setattr(a, name, kw.pop(name, M * (i + 1)))
+        assert not kw
+        return function(C.byref(a), *tail, None)
+
+    forward = lambda **kw: linear(B.LinearArgs, lib.smile_linear, (), **kw)                                       # noqa: E731
+    x, w, bias, residual, start, y, pre = (M * (i + 1) for i in range(7))
+    for wrong in (dict(y=x), dict(y=w + 16), dict(y=bias), dict(y=start), dict(y=residual + 16), dict(pre=y), dict(pre=x + 128), dict(pre=residual), dict(y=residual, pre=residual)):
+        assert forward(**wrong) == B.INVALID_ARG, wrong
+    backward = lambda **kw: linear(B.LinearBackwardArgs, lib.smile_linear_backward, (64 * M, BIG), **kw)          # noqa: E731
+    dy, x, w, pre, start, dx, dw, db = (M * (i + 1) for i in range(8))
+    for wrong in (dict(dx=dy), dict(dx=x + 16), dict(dx=w), dict(dx=pre), dict(dw=x), dict(dw=w), dict(dw=dx), dict(dbias=start), dict(dbias=dw + 1024), dict(dw=dy + 32)):
+        assert backward(**wrong) == B.INVALID_ARG, wrong
+        assert backward(act=0, **wrong) == B.INVALID_ARG, wrong
+    shared = adam()
+    for wrong in ([shared, shared], [shared, {**adam(), "param": shared["param"]}], [{**adam(), "m": shared["v"], "v": shared["v"]}],
+                  [shared, {**adam(), "m_scale": shared["v_scale"]}]):
+        with pytest.raises(B.SmileError) as e:
+            B.AdamW(wrong)
+        assert e.value.status == B.INVALID_ARG
+    B.AdamW([shared, {**adam(), "grad": shared["grad"]}])   # a gradient is only read
+
+
 def test_binding_refuses_shapes_and_types():
     f32, i32 = torch.float32, torch.int32
     z = torch.zeros
