@@ -80,7 +80,7 @@ def test_block_forward_and_backward(dtype, act, T, k, N, d, F, normalize, masked
             continue
         off = float((got.double() - ref).norm() / ref.norm())
         assert off <= TOL[dtype], (name, off)
-    assert abs(float(loss) - float(want_loss.detach())) <= 1e-4 * float(want_loss)
+    assert abs(float(loss) - float(want_loss.detach())) <= 1e-4 * float(want_loss.detach())
     count = torch.bincount(block.idx[block.idx >= 0].flatten().long(), minlength=N)
     assert torch.equal(block.count.long(), count) and int(block.start[-1]) == int(count.sum())
     block.close()
