@@ -11,7 +11,7 @@
 // What bounds it: the matrix cores, if what they are fed with keeps up.  A wave that reads its fragments (up to 16 of 16 bytes a lane) cannot multiply, so two waves
 // of a SIMD take turns (STAGGER): the waves are two halves, one a barrier behind the other; while one multiplies the other reads and requests.  With
 // four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.  On a full chip a slab of 256 x 256 takes 1.56 us (1380
-// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1080); an epilogue about 9 and 4 us, 16 and 6 with GELU.  8192^3: 797 us (1380 TFLOP/s).
+// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1080); an epilogue about 8 and 4 us, 13 and 6 with GELU.  8192^3: 797 us (1380 TFLOP/s).
 //
 // Operand units in LDS.  Normal: [row][64 k], piece c (16 bytes) of a row at c ^ ((row >> 1) & 7).  Transposed: as in memory, [64 k][columns], fragments by
 // transposing reads; pieces rotated by 4 (k & 3) in rows of 16 pieces, by 4 ((k >> 1) & 1) in rows of 8, so that successive k-rows fall on distinct banks.
@@ -389,13 +389,21 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
                 });
                 asm volatile("" ::: "memory");
             }
-            each_four([&](int, int, f32x4 v, auto at) __attribute__((always_inline)) {
-                vec4 r = vec4{(E)0.f, (E)0.f, (E)0.f, (E)0.f};
-                if (!GRAD && a.residual) r = *at;
+            // one branch for all of a block, not one for each four values, which keeps their chains apart (16384 rows 1024 -> 4096 with GELU: 164 -> 157 us; 64 groups 424 -> 411)
+            auto finish = [&](auto added) __attribute__((always_inline)) {
+                each_four([&](int, int, f32x4 v, auto at) __attribute__((always_inline)) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = linear_act<false>(ACT, v[k]) + (float)r[k];
-                *at = vec4{(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
-            });
+                    for (int k = 0; k < 4; ++k) v[k] = linear_act<false>(ACT, v[k]);
+                    if constexpr (decltype(added)::value) {
+                        const vec4 r = *at;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] += (float)r[k];
+                    }
+                    *at = vec4{(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
+                });
+            };
+            if (!GRAD && a.residual) finish(std::true_type{});
+            else finish(std::false_type{});
             store_staged(Y);
         });
         if (full) stores = TM * (!GRAD && a.pre ? 8 : 4);
