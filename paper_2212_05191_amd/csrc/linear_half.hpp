@@ -11,7 +11,7 @@
 // What bounds it: the matrix cores, if what they are fed with keeps up.  A wave that reads its fragments (up to 16 of 16 bytes a lane) cannot multiply, so two waves
 // of a SIMD take turns (STAGGER): the waves are two halves, one a barrier behind the other; while one multiplies the other reads and requests.  With
 // four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.  On a full chip a slab of 256 x 256 takes 1.56 us (1380
-// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1080); an epilogue about 8 and 4 us, 13 and 6 with GELU.  8192^3: 797 us (1380 TFLOP/s).
+// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1080); an epilogue about 7 and 4 us, 10 and 6 with GELU.  8192^3: 783 us (1404 TFLOP/s).
 //
 // Operand units in LDS.  Normal: [row][64 k], piece c (16 bytes) of a row at c ^ ((row >> 1) & 7).  Transposed: as in memory, [64 k][columns], fragments by
 // transposing reads; pieces rotated by 4 (k & 3) in rows of 16 pieces, by 4 ((k >> 1) & 1) in rows of 8, so that successive k-rows fall on distinct banks.
@@ -253,10 +253,17 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
                     for (int q = 0; q < QA; ++q) acc[i][P * QA + q] = Half<E>::mfma_32x32x16(i ? fb1[kk] : fb0[kk], fa[q][kk], acc[i][P * QA + q]);
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (STAGGER) {
+        if constexpr (STAGGER && P == 0) {
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    // The barrier behind a tile's last phase is what the later half owes until its epilogue is done: had it to meet the other half's next one in front of it, the two
+    // epilogues would follow each other (16384 rows 1024 -> 4096 with GELU: 160 -> 150 us; 64 groups 417 -> 395, 4096 -> 1024 without 303 -> 293).
+    bool owed = false;
+    auto pay = [&]() __attribute__((always_inline)) {
+        if (STAGGER && owed) __builtin_amdgcn_s_barrier();
+        owed = false;
     };
 
     lds_char *const stg = lds + 2 * STAGE + wave * 4096;
@@ -270,6 +277,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
         upper = t.rows > UA;
+        if (t.kv > 0) pay();
         int steady = 0;   // slabs to come that are
         for (int n_slabs = (t.kv + 63) / 64; n_slabs > 0; --n_slabs) {
             if (steady == 0 && fresh == 2 && !l_done) {   // (the slab requested in a slab's second phase is the one behind that of the first)
@@ -278,6 +286,11 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
             }
             const bool is_steady = steady > 0;
             phase(SMILE_IC(0), is_steady), phase(SMILE_IC(1), is_steady);
+            if constexpr (STAGGER) {
+                owed = n_slabs == 1 && wm == 1;
+                if (!owed) __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+            }
             steady = max(steady - 1, 0);
             fresh = min(fresh + 1, 2);
             c_stage ^= STAGE;
@@ -408,6 +421,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void linear_half_kernel(LinearGemm 
         });
         if (full) stores = TM * (!GRAD && a.pre ? 8 : 4);
     }
+    pay();
     if (any) {
         wait_vmcnt<0>();   // nothing of this workgroup reaches its LDS any more
         if (STAGGER && wm == 0) __builtin_amdgcn_s_barrier();
