@@ -31,20 +31,20 @@ hipError_t launch_typed(const LinearGemm &g, LinearKind kind, HalfTile tile, con
 // 256 x 256 outputs alone on a CU move half of the bytes from L2 that 128 x 128 do, but the epilogue waits for nobody and nobody multiplies meanwhile, and there
 // are a quarter as many tiles to spread.  Time of `tiles` tiles of `slabs` slabs, us: rounds of the chip, each slabs x time of a slab (shorter while CUs are idle) + what a
 // tile costs beside it; from two rounds on workgroups are out of step and share the last one.  Measured, bfloat16, 256 and 128 (in brackets the model):
-//   forward, 16384 rows 1024 -> 4096: 141 / 165 (143 / 170), with GELU 167 / 181 (170 / 189); 256 -> 4096: 71 / 67 (67 / 69), 98 / 87 (94 / 88)
-//   64 groups of 512 rows, 1024 -> 4096: 389 / 439 (349 / 376), GELU 418 / 440 (416 / 419); 16 groups of 512 rows, 768 -> 2304: 56 / 50 (61 / 51)
-//   gradient of x, 4096 rows, 4096 terms, 4096 columns: 116 / 137 (115 / 146), 1024 rows and columns in 32 / 64 tiles: 73 / 45 (77 / 47)
-//   gradient of the weights, 16384 x 4096 of 1024 rows: 129 / 154 (130 / 163); 2048 x 1024 of 4096 rows: 72 / 43 (74 / 46)
+//   forward, 16384 rows 1024 -> 4096: 125 / 156 (124 / 159), with GELU 146 / 170 (145 / 175); 256 -> 4096: 57 / 64 (52 / 63), 75 / 83 (73 / 79)
+//   64 groups of 512 rows, 1024 -> 4096: 363 / 431 (303 / 351), GELU 376 / 421 (355 / 387), 512 -> 1024 GELU: 70 / 59 (68 / 68); 16 groups, 768 -> 2304: 45 / 46 (53 / 47)
+//   gradient of x, 4096 rows, 4096 terms, 4096 columns: 108 / 130 (107 / 136), 1024 columns of 2048 rows: 69 / 44 (72 / 46)
+//   gradient of the weights, 16384 x 4096 of 1024 rows: 124 / 146 (123 / 153); 2048 x 1024 of 4096 rows: 70 / 43 (72 / 46)
 double linear_half_time(HalfTile tile, LinearKind kind, double tiles, double slabs, bool gelu)
 {
     auto shared = [](double n) { return n <= 2.0 ? std::ceil(n) : std::min(std::ceil(n), n + 0.25); };
     const double n = tiles / (tile == kHalf256 ? kLinearCus : 2 * kLinearCus), full = std::min(n, 1.0);
     if (tile == kHalf256) {
-        const double beside = kind == kLinearWeightGrad ? 6.0 : kind == kLinearRowGrad ? 8.5 : gelu ? 16.0 : 9.3;
-        return 5.0 + shared(n) * ((0.95 + 0.62 * full * full) * slabs + beside);
+        const double beside = kind == kLinearWeightGrad ? 5.4 : kind == kLinearRowGrad ? 5.5 : gelu ? 11.0 : 5.8;
+        return 5.0 + shared(n) * ((0.92 + 0.58 * full * full) * slabs + beside);
     }
-    const double beside = kind == kLinearWeightGrad ? 3.0 : kind == kLinearRowGrad ? 3.5 : gelu ? 6.2 : 3.8;
-    return 5.0 + shared(n) * ((0.59 + 0.46 * full * full) * slabs + (n <= 1.0 ? 0.5 : 1.0) * beside);
+    const double beside = kind == kLinearWeightGrad ? 2.5 : kind == kLinearRowGrad ? 2.5 : gelu ? 5.2 : 3.2;
+    return 5.0 + shared(n) * ((0.59 + 0.41 * full * full) * slabs + (n <= 1.0 ? 0.5 : 1.0) * beside);
 }
 
 // Groups of unknown rows are taken as even, with half a tile more each

@@ -10,8 +10,8 @@
 //
 // What bounds it: the matrix cores, if what they are fed with keeps up.  A wave that reads its fragments (up to 16 of 16 bytes a lane) cannot multiply, so two waves
 // of a SIMD take turns (STAGGER): the waves are two halves, one a barrier behind the other; while one multiplies the other reads and requests.  With
-// four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.  On a full chip a slab of 256 x 256 takes 1.56 us (1380
-// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1080); an epilogue about 7 and 4 us, 10 and 6 with GELU.  8192^3: 783 us (1404 TFLOP/s).
+// four waves (128 x 128 tiles, two workgroups on a CU) the workgroups do so by themselves, at one barrier a phase.  On a full chip a slab of 256 x 256 takes 1.5 us (1430
+// TFLOP/s between epilogues), of 128 x 128 two on a CU 1.0 (1070); an epilogue about 5.5 and 3 us, 11 and 5 with GELU.  8192^3: 783 us (1404 TFLOP/s).
 //
 // Operand units in LDS.  Normal: [row][64 k], piece c (16 bytes) of a row at c ^ ((row >> 1) & 7).  Transposed: as in memory, [64 k][columns], fragments by
 // transposing reads; pieces rotated by 4 (k & 3) in rows of 16 pieces, by 4 ((k >> 1) & 1) in rows of 8, so that successive k-rows fall on distinct banks.
