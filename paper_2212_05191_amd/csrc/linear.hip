@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void linear_row_sum_kernel(const float *partia
 struct GradPlan {
     int chunk, parts;         // weights: rows of a part (0: whole groups), parts of all groups
     int x_chunk, x_parts;     // rows: terms of a part, parts
-    HalfTile tile;            // weights, 16-bit types
+    HalfTile tile, x_tile;    // of the weights' gradient and the rows', 16-bit types
     size_t sums_at, partial_at, total;
 };
 constexpr int kMostParts = 16;
@@ -140,7 +140,7 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
         return half ? linear_half_time(size == 256 ? kHalf256 : kHalf128, kind, tiles, slabs, false) : linear_half_time(kHalf128, kind, tiles / 2, 1.5 * slabs, false);
     };
     auto tiles_of = [](int n, int size) { return (n + size - 1) / size; };
-    p.parts = a.N, p.tile = kHalf128;
+    p.parts = a.N, p.tile = p.x_tile = kHalf128;
     if (a.dw) {
         const double elements = (double)a.N * a.F * a.K;
         double best = 1e30;
@@ -160,13 +160,17 @@ GradPlan grad_plan(const smile_linear_backward_args &a)
     }
     p.x_parts = 1;
     if (a.dx) {
-        const int size = half ? 128 : kF32Tile, slabs = tiles_of(a.F, 64);
-        const double per = (double)a.rows / a.N, tiles = (a.N == 1 ? std::ceil(per / size) : std::min((double)a.rows, a.N * std::max(1.0, per / size + 0.5))) * tiles_of(a.K, size);
-        double best = time(kLinearRowGrad, size, tiles, slabs);
+        const int slabs = tiles_of(a.F, 64);
+        const double per = (double)a.rows / a.N;
+        double best = 1e30;
         int cuts = 1;
-        for (int n = 2; n <= kMostParts && 4 * n <= slabs; ++n) {
-            const double t = time(kLinearRowGrad, size, tiles * n, tiles_of(slabs, n)) + parts_time(n, (double)a.rows * a.K);
-            if (t < best) best = t, cuts = n;
+        for (const int size : {half ? 128 : kF32Tile, 256}) {
+            if (!half && size == 256) break;
+            const double tiles = (a.N == 1 ? std::ceil(per / size) : std::min((double)a.rows, a.N * std::max(1.0, per / size + 0.5))) * tiles_of(a.K, size);
+            for (int n = 1; n <= kMostParts && (n == 1 || 4 * n <= slabs); ++n) {
+                const double t = time(kLinearRowGrad, size, tiles * n, tiles_of(slabs, n)) + parts_time(n, (double)a.rows * a.K);
+                if (t < best) best = t, cuts = n, p.x_tile = size == 256 ? kHalf256 : kHalf128;
+            }
         }
         if (cuts > 1) {
             p.x_chunk = tiles_of(slabs, cuts) * 64;
@@ -194,14 +198,13 @@ hipError_t launch_f32(LinearGemm g, const Tuning &tune, hipStream_t s)
 }
 
 template <typename E, bool GRAD, bool WT>
-hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s, const HalfTile *tile = nullptr)
+hipError_t launch_product(const LinearGemm &g, const Tuning &tune, hipStream_t s, HalfTile tile = kHalf128)
 {
     if constexpr (sizeof(E) == 4) return launch_f32<E, GRAD, WT>(g, tune, s);
     else {
         const int dtype = std::is_same_v<E, __bf16> ? SMILE_DTYPE_BF16 : SMILE_DTYPE_F16;
-        if (!WT && linear_few_applies(g)) return launch_linear_few(dtype, g, tune, s);
-        const LinearKind kind = GRAD ? kLinearWeightGrad : WT ? kLinearRowGrad : kLinearForward;
-        return launch_linear_half(dtype, g, kind, tile ? *tile : pick_half_tile(kind, g), tune, s);
+        if (WT) return launch_linear_half(dtype, g, GRAD ? kLinearWeightGrad : kLinearRowGrad, tile, tune, s);   // (the gradients' tiles go with their parts)
+        return linear_few_applies(g) ? launch_linear_few(dtype, g, tune, s) : launch_linear_half(dtype, g, kLinearForward, forward_half_tile(g), tune, s);
     }
 }
 
@@ -234,7 +237,7 @@ hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, voi
         m.x = g, m.w = a.w, m.y = a.dx, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Nout = a.K, m.K = a.F, m.ldx = a.F, m.ldw = a.K;
         m.sw = (long long)a.F * a.K, m.sy = (long long)a.rows * a.K, m.chunk = p.x_chunk, m.parts = p.x_parts;
         if (p.x_parts > 1) m.partial = reinterpret_cast<float *>(ws + p.partial_at);
-        const hipError_t err = launch_product<E, false, true>(m, tune, s);
+        const hipError_t err = launch_product<E, false, true>(m, tune, s, p.x_tile);
         if (err != hipSuccess) return err;
         if (p.x_parts > 1)
             SMILE_LAUNCH(linear_row_sum_kernel<E>, dim3((unsigned)((m.sy + 1023) / 1024)), dim3(256), 0, s, (const float *)m.partial, a.start, static_cast<E *>(a.dx), a.N, a.rows,
@@ -245,7 +248,7 @@ hipError_t backward(const smile_linear_backward_args &a, const Tuning &tune, voi
         m.x = g, m.w = a.x, m.y = a.dw, m.start = a.start, m.N = a.N, m.rows = a.rows, m.Mrows = a.F, m.Nout = a.K, m.ldx = a.F, m.ldw = a.K;
         m.sy = (long long)a.F * a.K, m.chunk = p.chunk, m.parts = p.parts;
         if (p.chunk) m.partial = reinterpret_cast<float *>(ws + p.partial_at);
-        const hipError_t err = launch_product<E, true, true>(m, tune, s, &p.tile);
+        const hipError_t err = launch_product<E, true, true>(m, tune, s, p.tile);
         if (err != hipSuccess) return err;
         if (p.chunk)
             SMILE_LAUNCH(linear_part_sum_kernel<E>, dim3((unsigned)((m.sy + 1023) / 1024), a.N), dim3(256), 0, s, (const float *)m.partial, a.start, static_cast<E *>(a.dw),

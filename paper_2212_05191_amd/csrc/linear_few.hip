@@ -29,14 +29,15 @@ hipError_t launch_typed(const LinearGemm &g, int rows, const Tuning &tune, hipSt
 
 // Estimated times, us.  Measured with bfloat16 and GELU in a graph, this kernel and the tiles of 128 x 128: 1024 -> 4096, 1 row 3.8 / 13.7, 16 4.5 / 13.8, 32 5.5 / 14.0,
 // 64 7.5 / 13.9, 128 11.9 / 17.0, 256 21.4 / 17.2, 512 40 / 17.6; 4096 -> 1024, 16 rows 9.6 / 38, 64 20.2 / 38, 256 21.3 / 45, 512 38.5 / 45; 256 -> 256, 256 rows 4.0 / 9.7;
-// 64 groups 1024 -> 4096, 16 rows in all 21.3 / 21.8, 128 97 / 90, 1024 225 / 104 (the weights' bytes 26, 103, 103).  Here a workgroup's time goes with its rows and terms,
+// 64 groups 1024 -> 4096, 16 rows in all 21.3 / 21.8, 128 97 / 90, 1024 225 / 104 (the weights' bytes 26, 103, 103); 16 groups 768 -> 2304, 1024 rows 53 / 20; 8 groups
+// 256 -> 512, 2000 rows 11.5 / 9.1.  Here a workgroup's time goes with its rows and terms,
 // and the workgroups share the CUs; there a slab costs 0.6 us as long as the tiles do not fill the chip.
 bool linear_few_applies(const LinearGemm &g)
 {
     const int rows = few_rows(g), size = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     const double k = g.K / 1024.0, cost = size == 16 ? 1.6 : size == 32 ? 2.5 : 4.3;
     const double here = row_tiles(g, size) * ((g.Nout + 15) / 16) / kLinearCus, tiles = row_tiles(g, 128) * ((g.Nout + 127) / 128) / (1.5 * kLinearCus);
-    return 3.2 + cost * k * std::max(1.0, here) < 6.0 + 9.6 * k * std::max(1.0, tiles);
+    return 3.2 + cost * (k + 0.1) * std::max(1.0, here) < 6.0 + 9.6 * k * std::max(1.0, tiles);
 }
 
 hipError_t launch_linear_few(int dtype, const LinearGemm &g, const Tuning &tune, hipStream_t s)

@@ -44,18 +44,18 @@ double linear_half_time(HalfTile tile, LinearKind kind, double tiles, double sla
         return 5.0 + shared(n) * ((0.92 + 0.58 * full * full) * slabs + beside);
     }
     const double beside = kind == kLinearWeightGrad ? 2.5 : kind == kLinearRowGrad ? 2.5 : gelu ? 5.2 : 3.2;
-    return 5.0 + shared(n) * ((0.59 + 0.41 * full * full) * slabs + (n <= 1.0 ? 0.5 : 1.0) * beside);
+    // (up to half of the slots: one workgroup on a CU)
+    return 5.0 + shared(n) * ((n <= 0.5 ? 0.59 + 0.41 * n * n : 1.0) * slabs + (n <= 1.0 ? 0.5 : 1.0) * beside);
 }
 
 // Groups of unknown rows are taken as even, with half a tile more each
-HalfTile pick_half_tile(LinearKind kind, const LinearGemm &g)
+HalfTile forward_half_tile(const LinearGemm &g)
 {
     auto time = [&](HalfTile tile) {
         const int size = tile == kHalf256 ? 256 : 128;
         const double cols = (g.Nout + size - 1) / size, per = (double)g.rows / g.N;
-        if (kind == kLinearWeightGrad) return linear_half_time(tile, kind, (double)g.parts * ((g.Mrows + size - 1) / size) * cols, std::ceil((double)g.rows / g.parts / 64), false);
         const double tiles = g.N == 1 ? std::ceil(per / size) : std::min((double)g.rows, g.N * std::max(1.0, per / size + 0.5));
-        return linear_half_time(tile, kind, g.parts * tiles * cols, std::ceil((double)g.K / g.parts / 64), g.act == 2);
+        return linear_half_time(tile, kLinearForward, tiles * cols, (g.K + 63) / 64, g.act == 2);
     };
     return time(kHalf256) <= time(kHalf128) ? kHalf256 : kHalf128;
 }

@@ -28,7 +28,7 @@ enum LinearKind { kLinearForward, kLinearRowGrad, kLinearWeightGrad };
 enum HalfTile { kHalf256, kHalf128 };
 // what the choice of a tile and the cuts of the gradients' sums go by: their workspace is asked for on the host alone
 constexpr int kLinearCus = 256;
-HalfTile pick_half_tile(LinearKind kind, const LinearGemm &g);
+HalfTile forward_half_tile(const LinearGemm &g);
 double linear_half_time(HalfTile tile, LinearKind kind, double tiles, double slabs, bool gelu);   // estimated, us
 hipError_t launch_linear_half(int dtype, const LinearGemm &g, LinearKind kind, HalfTile tile, const Tuning &tune, hipStream_t s);
 
