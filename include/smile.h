@@ -496,7 +496,7 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
  * one.  The functions ending in _bytes, and smile_adamw_plan, work on the host alone.
  * What a call writes must not overlap what it reads or writes besides, but where a tensor may be another: SMILE_INVALID_ARG.
  * Limits: T, rows, N, k, d, K, F >= 1; N <= 4096; k <= N and k <= 64; T*k < 2^26, rows and R <= 2^27; d, K, F % 8 == 0; d <= 16384,
- * K, F <= 32768; elements of any tensor below 2^40.
+ * K, F <= 32768; elements of any tensor below 2^40; rows * N of a product below 2^36.
  * Indices and row numbers are never followed outside their tensors: a pair whose expert is not in 0 .. N - 1 has no row, a row number that is not in
  * 0 .. R - 1 counts as none, and first rows are taken as what lies in order within 0 .. rows.
  * ------------------------------------------------------------------------- */

@@ -17,6 +17,7 @@ namespace {
 constexpr int kWidest = 32768, kWidestRow = 16384, kMostExperts = 4096, kMostChoices = 64;
 constexpr long long kMostRows = 1ll << 27, kMostPairs = 1ll << 26;
 constexpr double kMostElements = 1099511627776.0;   // 2^40
+constexpr double kMostGroupRows = 68719476736.0;    // 2^36: first rows that each let a group begin at row 0 still add up to less than 2^31 tiles of 64 rows
 
 bool known(int dtype) { return dtype == SMILE_DTYPE_F32 || dtype == SMILE_DTYPE_BF16 || dtype == SMILE_DTYPE_F16; }
 bool known_act(int act) { return act == SMILE_ACT_NONE || act == SMILE_ACT_RELU || act == SMILE_ACT_GELU; }
@@ -69,6 +70,7 @@ smile_status check_linear(int N, int rows, int K, int F, int dtype, int act, con
     if (N < 1 || N > kMostExperts || rows < 1 || rows > kMostRows) return SMILE_BAD_SHAPE;
     if (K < 8 || K % 8 || K > kWidest || F < 8 || F % 8 || F > kWidest) return SMILE_BAD_SHAPE;
     if ((double)rows * std::max(K, F) >= kMostElements || (double)N * K * F >= kMostElements) return SMILE_BAD_SHAPE;
+    if ((double)rows * N >= kMostGroupRows) return SMILE_BAD_SHAPE;
     return N > 1 && !start ? SMILE_INVALID_ARG : SMILE_OK;
 }
 

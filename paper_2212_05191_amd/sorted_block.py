@@ -5,7 +5,7 @@ fixed capacity.
     down-projection with bias, weighted return, added to the residual stream
 
 the gradients of all of it, with a load-balancing term, and an AdamW step over the experts and the router.  Marshalling only: every step is a library call, no tensor is
-allocated after construction, and nothing depends on the host: forward, backward and step can be captured into a graph.
+allocated after construction (but the value of loss()), and nothing depends on the host: forward, backward and step can be captured into a graph.
 
     python -m paper_2212_05191_amd.sorted_block     # a training step at the base layer's size, timed, beside the layer with capacity buffers
 """

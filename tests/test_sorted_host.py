@@ -105,7 +105,7 @@ def test_linear_refusals():
     assert need(w=None, dx=None) == B.OK and need(x=None, dw=None) == B.OK and need(pre=None, act=2) == B.OK
     for f in (call, back, need):
         for bad in (dict(N=0), dict(N=4097), dict(rows=0), dict(rows=(1 << 27) + 1), dict(K=0), dict(K=12), dict(K=32776), dict(F=0), dict(F=20), dict(F=32776),
-                    dict(rows=1 << 27, K=16384), dict(N=4096, K=32768, F=32768)):
+                    dict(rows=1 << 27, K=16384), dict(N=4096, K=32768, F=32768), dict(rows=1 << 24, N=4096), dict(rows=1 << 27, N=512)):
             assert f(**bad) == B.BAD_SHAPE, bad
         assert f(dtype=3) == B.UNSUPPORTED and f(dtype=-1) == B.UNSUPPORTED and f(act=3) == B.UNSUPPORTED and f(act=-1) == B.UNSUPPORTED
     assert need() == B.OK and size.value > 0
