@@ -9,7 +9,8 @@ namespace smile {
 
 namespace {
 
-constexpr int kGradRows = 128;       // rows of a part of the bias gradient's sums
+// rows of a part of the bias gradient's sums: 16384 rows of 1024 values take 12.4 us by 128, 9.2 by 64, 8.0 by 32, their sums 4.0, 4.4 and 7.7 more
+constexpr int kGradRows = 64;
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
