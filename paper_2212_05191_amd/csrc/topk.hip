@@ -16,8 +16,9 @@ namespace {
 
 // Workgroups of the choice: more of them make more partial sums, fewer leave the CUs short of waves (65536 x 128, k = 8: 512 31 us, 1024 25, 2048 25 and a longer sum)
 constexpr int kThreads = 256, kMaxBlocks = 1024;
-// tokens that one workgroup takes alone, without a second launch for p_sum: lanes of work
-constexpr int kAloneLanes = 4 * kThreads;
+// tokens that one workgroup takes alone, without a second launch for p_sum: rounds of its lanes.  The launch costs 2 to 3 us; a second round 1 (64 tokens of 24: 4.5 us against
+// 5.5), of more columns 3 to 9 (16 of 256: 9.2 against 8.0; 8 of 4096: 27.7 against 18.3).
+constexpr int alone_lanes(int N) { return (N <= 64 ? 2 : 1) * kThreads; }
 
 // Reductions over the L lanes of a token (L = 4 .. 64, aligned); every lane ends with the same bits
 template <int CTRL>
@@ -318,12 +319,21 @@ __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 2 : 
     }
 }
 
-// f(lanes, values) of the smallest shape that holds N columns
+// f(lanes, values) of the smallest shape that holds N columns.  Few tokens leave lanes idle and their time is that of a lane's values one after another: twice the
+// lanes with half of the values (choice with sum, gradient; 1 token of 128, k = 8: 7.0 -> 4.8, 5.4 -> 3.7 us; 8192: 11.4 -> 9.2, 6.1 -> 4.8; many repeat less with
+// fewer lanes: 65536 27.7 against 31.1).
 template <typename F>
-auto with_shape(int N, F &&f)
+auto with_shape(int T, int N, F &&f)
 {
 #define SMILE_SHAPE(l, v) return f(std::integral_constant<int, l>{}, std::integral_constant<int, v>{})
     if (N <= 16) SMILE_SHAPE(4, 4);
+    if ((long long)T * N <= 1 << 20) {
+        if (N <= 32) SMILE_SHAPE(8, 4);
+        if (N <= 64) SMILE_SHAPE(16, 4);
+        if (N <= 128) SMILE_SHAPE(16, 8);
+        if (N <= 256) SMILE_SHAPE(32, 8);
+        if (N <= 512) SMILE_SHAPE(64, 8);
+    }
     if (N <= 32) SMILE_SHAPE(4, 8);
     if (N <= 64) SMILE_SHAPE(8, 8);
     if (N <= 128) SMILE_SHAPE(8, 16);
@@ -335,13 +345,13 @@ auto with_shape(int N, F &&f)
 #undef SMILE_SHAPE
 }
 
-int lanes(int N) { return with_shape(N, [](auto l, auto) { return (int)decltype(l)::value; }); }
+int lanes(int T, int N) { return with_shape(T, N, [](auto l, auto) { return (int)decltype(l)::value; }); }
 
 // tokens of a workgroup (a whole number of rounds of its lanes) and workgroups
-void plan(int T, int N, int &per_block, int &blocks)
+void plan(int T, int N, bool sum, int &per_block, int &blocks)
 {
-    const int tpb = kThreads / lanes(N);
-    if ((long long)T * lanes(N) <= kAloneLanes) {
+    const int tpb = kThreads / lanes(T, N);
+    if (sum && (long long)T * lanes(T, N) <= alone_lanes(N)) {
         per_block = T, blocks = 1;
         return;
     }
@@ -355,7 +365,7 @@ void plan(int T, int N, int &per_block, int &blocks)
 size_t topk_workspace(int T, int N)
 {
     int per_block, blocks;
-    plan(T, N, per_block, blocks);
+    plan(T, N, true, per_block, blocks);
     return blocks > 1 ? (size_t)blocks * N * sizeof(float) : 0;
 }
 
@@ -363,9 +373,9 @@ hipError_t launch_topk(const TopkIo &given, hipStream_t s)
 {
     TopkIo io = given;
     int per_block, blocks;
-    plan(io.T, io.N, per_block, blocks);
+    plan(io.T, io.N, io.p_sum != nullptr, per_block, blocks);
     if (!io.p_sum || blocks == 1) io.partial = nullptr;
-    with_shape(io.N, [&](auto l, auto v) {
+    with_shape(io.T, io.N, [&](auto l, auto v) {
         SMILE_LAUNCH((topk_kernel<decltype(l)::value, decltype(v)::value>), dim3(blocks), dim3(kThreads), 0, s, io, per_block);
         return 0;
     });
@@ -375,7 +385,7 @@ hipError_t launch_topk(const TopkIo &given, hipStream_t s)
 
 hipError_t launch_topk_backward(const TopkGradIo &io, hipStream_t s)
 {
-    with_shape(io.N, [&](auto l, auto v) {
+    with_shape(io.T, io.N, [&](auto l, auto v) {
         const int tpb = kThreads / decltype(l)::value;
         SMILE_LAUNCH((topk_backward_kernel<decltype(l)::value, decltype(v)::value>), dim3((io.T + tpb - 1) / tpb), dim3(kThreads), 0, s, io);
         return 0;

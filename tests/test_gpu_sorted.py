@@ -62,7 +62,8 @@ def run_topk(logits, k, bias=None, normalize=False, p_sum=True):
 
 
 SHAPES = [(1, 1, 1), (1, 64, 2), (3, 5, 5), (7, 16, 16), (33, 17, 3), (65, 33, 8), (130, 64, 8), (257, 100, 6), (1000, 128, 8), (300, 129, 64), (77, 256, 1),
-          (50, 300, 2), (20, 513, 33), (9, 1025, 64), (5, 2049, 7), (3, 4096, 64), (4097, 8, 2)]
+          (50, 300, 2), (20, 513, 33), (9, 1025, 64), (5, 2049, 7), (3, 4096, 64), (4097, 8, 2),
+          (35001, 31, 3), (17003, 63, 9), (9001, 128, 8), (8999, 127, 17), (4500, 256, 33), (2101, 511, 40)]
 
 
 @pytest.mark.parametrize("normalize", (False, True))
