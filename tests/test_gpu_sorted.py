@@ -192,7 +192,7 @@ def test_balance_term_of_nearly_even_counts():
 # ------------------------------------------------------------------ sort
 
 @pytest.mark.parametrize("T,k,N", [(1, 1, 1), (3, 2, 5), (16, 2, 64), (1000, 3, 7), (2048, 2, 4), (2049, 2, 255), (700, 8, 257), (5003, 2, 15), (900, 5, 1024),
-                                   (1500, 4, 1025), (300, 16, 4096), (40000, 4, 64)])
+                                   (1500, 4, 1025), (300, 16, 4096), (40000, 4, 64), (1025, 1, 9), (6001, 4, 300), (6001, 4, 1030), (11003, 2, 4095), (12001, 4, 4096)])
 def test_sort_experts(T, k, N):
     g = gen(T + N)
     idx = torch.randint(0, N, (T, k), generator=g, device=DEV, dtype=torch.int32)
