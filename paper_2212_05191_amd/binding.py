@@ -658,17 +658,26 @@ def _nbytes(t):
     return 0 if t is None else t.numel() * t.element_size()
 
 
+_int32 = _current_device = None     # torch's, once it is imported: looking them up costs as much as a check
+
+
 def _i32():
-    import torch
-    return torch.int32
+    global _int32
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    return _int32
 
 
 def _check_device(*tensors):
     """Tensors of the current device: a kernel would follow any other pointer blindly."""
-    import torch
-    here = torch.cuda.current_device()
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = torch.cuda.current_device
+    here = _current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
+        if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
 
 
