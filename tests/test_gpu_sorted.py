@@ -404,6 +404,16 @@ def test_linear_of_many_rows(name, N, rows, K, F, behind, skew, dtype):
     run_linear_backward(g, x, w, kept if name != "none" else None, name, start, live, dtype)
 
 
+@pytest.mark.parametrize("first", ([0, 0, 0, 6000, 6000, 6001, 15000, 15000, 15500, 15500], [0, 15500, 15500, 15500, 15500, 15500, 15500, 15500, 15500, 15500],
+                                   [40, 40, 40, 40, 40, 40, 40, 40, 40, 15500], [7, 7, 7, 7, 7, 7, 7, 7, 7, 7]))
+def test_linear_of_many_rows_in_few_groups(first):
+    """Tiles without a term among others, at the beginning and at the end of a workgroup's"""
+    g = gen(first[3] + first[-1])
+    start = torch.tensor(first, dtype=torch.int32, device=DEV)
+    x, w, b, res, y, kept, live = run_linear(g, 9, 15500, 2056, 1544, "bf16", "gelu", True, False, start, pre=True, poison=True)
+    run_linear_backward(g, x, w, kept, "gelu", start, live, "bf16")
+
+
 @pytest.mark.parametrize("dtype", ("bf16", "f16"))
 def test_weights_gradient_of_many_rows_in_parts(dtype):
     """16000 rows in two parts of 256 x 256 tiles, their sums joined"""
