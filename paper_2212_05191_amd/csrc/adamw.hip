@@ -69,7 +69,8 @@ __device__ __forceinline__ int m_exponent(float largest)
     return max(__builtin_amdgcn_frexp_expf(largest) - 9 + (f > 0.875f ? 1 : 0), -126);
 }
 
-// ---- the second moment: codes of 5 exponent and 3 fraction bits, code 8 (x + 30) + f for (1 + f / 8) 2^x of the block's power of two.  v finite.
+// ---- the second moment: codes of 5 exponent and 3 fraction bits, code 8 (x + 30) + f for (1 + f / 8) 2^x of the block's power of two, at most 248 (its
+// double); 255 is infinity.  v finite.
 __device__ __forceinline__ uint32_t v_code(float v, int e, uint32_t r)
 {
     const float u = __builtin_amdgcn_ldexpf(v, -e);         // below 2; what is so small that it loses bits here gets the least code
@@ -83,7 +84,8 @@ __device__ __forceinline__ int v_exponent(float largest)
 
 // values of eight codes, before the block's power of two; and after
 __device__ __forceinline__ void m_units(uint2 codes, float *m) { unpack4(codes.x, 1.f, m), unpack4(codes.y, 1.f, m + 4); }
-__device__ __forceinline__ float v_unit(uint32_t c) { return c == 0 ? 0.f : __uint_as_float((c + ((127u - 30u) << 3)) << 20); }
+// (infinity: the square of a finite gradient may be that, and its m is not.  Were v as small as its neighbours from the next step on, m would be divided by almost nothing.)
+__device__ __forceinline__ float v_unit(uint32_t c) { return __uint_as_float(c - 1u < 248u ? (c + ((127u - 30u) << 3)) << 20 : c << 23); }   // 255 << 23: infinity
 __device__ __forceinline__ void v_units(uint2 codes, float *v)
 {
 #pragma unroll
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void adamw_kernel(AdamwStep a)
                     top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu), top_v = max(top_v, __float_as_uint(v[i]) & 0x7fffffffu);
                 }
                 top_m = block_max(top_m), top_v = block_max(top_v);
-                uint32_t odd = 0u;                 // elements of a gradient that is not finite: their codes are set below
+                uint32_t odd = 0u;                 // elements that are not finite: their codes are set below
                 if (max(top_m, top_v) >= kInfinity) {
                     top_m = top_v = 0u;
 #pragma unroll

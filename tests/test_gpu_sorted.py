@@ -738,3 +738,27 @@ def test_captured_step_follows_its_inputs():
             rows = int(eager["start"][-1]) if name == "xs" else None
             assert torch.equal(eager[name][:rows], captured[name][:rows]), (i, name)
     assert int(eager["step"]) == 4
+
+
+# ------------------------------------------------------------------ at the ends of the ranges
+
+@pytest.mark.parametrize("bits", (8, 32))
+@pytest.mark.parametrize("dtype,value", [("f32", 1e21), ("f32", -1e30), ("bf16", 3e38)])
+def test_adamw_of_a_gradient_whose_square_is_infinite(dtype, value, bits):
+    """v is infinite, in the state too, and m is not: the element's update is 0 in this step and in those that follow, whatever the others' moments are"""
+    n, hit = 300, 140
+    t = adam_tensors(gen(1), [n], dtype, dtype, bits, False, False)[0]
+    rest = torch.arange(n, device=DEV) != hit
+    opt, step = B.AdamW([t], **BETAS), ints(1, value=1000)
+    keep = t["param"].clone()
+    for g in (value, 0.0, 1e-3, 0.0):
+        t["grad"][hit] = g
+        B.smile_adamw(opt, torch.full((1,), 1e-2, device=DEV), step)
+        m, v = t["m"], t["v"]
+        if bits == 8:
+            m, v = torch.full((384,), math.nan, device=DEV), torch.full((384,), math.nan, device=DEV)
+            B.smile_adamw_unpack_states(t["m"], t["m_scale"], t["v"], t["v_scale"], m, v)
+        assert float(t["param"][hit]) == float(keep[hit]), g
+        assert float(v[hit]) == math.inf and bool(m.isfinite().all()), g
+        # the others' power of two goes by the finite ones alone: at most 448 2^(111 - 127) at the start, and squares of gradients below 1
+        assert bool((v[:n][rest] <= 2.0 ** 4).all()) and bool(t["param"].isfinite().all()), g
