@@ -125,6 +125,14 @@ __device__ __forceinline__ void store_codes(void *base, size_t at, const uint32_
     __builtin_nontemporal_store((uint64_t)c[1] << 32 | c[0], reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(base) + at));
 }
 
+// The root's instruction takes what lies below the normal range as 0: such values are scaled by 2^64 on the way.
+__device__ __forceinline__ float root(float x)
+{
+    const bool small = x < 1.17549435e-38f;
+    const float r = __builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(x, small ? 64 : 0));
+    return small ? r * 2.32830644e-10f : r;
+}
+
 struct AdamwStep {
     int32_t *arrived;               // workgroups that have read the step number
     const AdamwTensor *tensors;
@@ -215,7 +223,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void adamw_kernel(AdamwStep a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 moments(a, g[i], m[i], v[i]);
-                const float update = m[i] * inv1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inv2) + a.eps);
+                const float update = m[i] * inv1 * __builtin_amdgcn_rcpf(root(v[i] * inv2) + a.eps);
                 p[i] -= lr * fmaf(decay, p[i], update);
             }
             store8<DT>(x.param, at, live, p);

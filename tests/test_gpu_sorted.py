@@ -762,3 +762,22 @@ def test_adamw_of_a_gradient_whose_square_is_infinite(dtype, value, bits):
         assert float(v[hit]) == math.inf and bool(m.isfinite().all()), g
         # the others' power of two goes by the finite ones alone: at most 448 2^(111 - 127) at the start, and squares of gradients below 1
         assert bool((v[:n][rest] <= 2.0 ** 4).all()) and bool(t["param"].isfinite().all()), g
+
+
+@pytest.mark.parametrize("size", (1e-18, 1e-19, 3e-20))
+def test_adamw_of_second_moments_below_the_normal_range(size):
+    """v of 1e-38 to 1e-41, whose root is far above a small eps"""
+    g = gen(3)
+    n = 5000
+    t = dict(param=normal(g, n), grad=normal(g, n).abs() * size + size, m=torch.zeros(n, device=DEV), v=torch.zeros(n, device=DEV))
+    p0, eps = t["param"].double(), 2.0 ** -100
+    lr = torch.full((1,), 1e-2, device=DEV)
+    B.smile_adamw(B.AdamW([t], beta1=0.9, beta2=0.99, eps=eps), lr, ints(1, value=99))
+    m, v = t["m"].double(), t["v"].double()
+    near(m, 0.1 * t["grad"].double(), t["grad"].double() * R.E32, "m")
+    near(v, 0.01 * t["grad"].double() ** 2, t["grad"].double() ** 2 * 0.01 * 6 * R.E32 + 4 * 2.0 ** -149, "v")
+    # from the moments as they are stored: the quotient's dozen roundings, and half a step of 2^-149 of v / (1 - beta2^t), of which the root takes half
+    c2 = 1 - 0.99 ** 100
+    update = m / (1 - 0.9 ** 100) / (torch.sqrt(v / c2) + eps)
+    tol = float(lr) * update * (16 * R.E32 + 2.0 ** -150 / (v / c2) / 2) + 4 * R.E32 * p0.abs()
+    near(t["param"], p0 - float(lr) * update, tol, "param")
