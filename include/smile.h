@@ -609,7 +609,7 @@ typedef struct smile_adamw_args {
     int32_t state_bits;          /* 32 or 8 */
     int32_t has_master;
     int32_t seed;
-    double beta1, beta2, eps;    /* 0 <= beta < 1, 0 < eps <= 1; 1 - beta is taken in 64 bits */
+    double beta1, beta2, eps;    /* 0 <= beta < 1, 2^-126 <= eps <= 1; 1 - beta is taken in 64 bits */
     int64_t chunks;              /* filled in by smile_adamw_plan */
 } smile_adamw_args;
 smile_status smile_adamw_plan_bytes(const smile_adamw_args *args, const smile_adamw_tensor *tensors, size_t *bytes);

@@ -1,6 +1,7 @@
 // C-ABI entry points of the operators of a layer without dropped tokens and of its optimizer: argument checks, all of them on the host before anything is
 // enqueued, and the plan of an optimizer step.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
@@ -90,7 +91,9 @@ smile_status check_adamw(const smile_adamw_args &a)
     if (a.tensors < 1 || a.tensors > 1 << 24) return SMILE_BAD_SHAPE;
     if (!known(a.dtype) || (a.grad_dtype != a.dtype && a.grad_dtype != SMILE_DTYPE_F32)) return SMILE_UNSUPPORTED;
     if ((a.state_bits != 32 && a.state_bits != 8) || (a.has_master && a.dtype == SMILE_DTYPE_F32)) return SMILE_UNSUPPORTED;
-    if (!(a.beta1 >= 0.0 && a.beta1 < 1.0 && a.beta2 >= 0.0 && a.beta2 < 1.0 && a.eps > 0.0 && a.eps <= 1.0)) return SMILE_BAD_SHAPE;
+    if (!(a.beta1 >= 0.0 && a.beta1 < 1.0 && a.beta2 >= 0.0 && a.beta2 < 1.0)) return SMILE_BAD_SHAPE;
+    // (below fp32's normal range a reciprocal is infinite, and an element without gradient and moments would be 0 times that)
+    if (!(a.eps <= 1.0 && (float)a.eps >= FLT_MIN)) return SMILE_BAD_SHAPE;
     return SMILE_OK;
 }
 

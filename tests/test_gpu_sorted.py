@@ -781,3 +781,14 @@ def test_adamw_of_second_moments_below_the_normal_range(size):
     update = m / (1 - 0.9 ** 100) / (torch.sqrt(v / c2) + eps)
     tol = float(lr) * update * (16 * R.E32 + 2.0 ** -150 / (v / c2) / 2) + 4 * R.E32 * p0.abs()
     near(t["param"], p0 - float(lr) * update, tol, "param")
+
+
+@pytest.mark.parametrize("eps", (2.0 ** -126, 1e-30))
+def test_adamw_of_the_least_eps(eps):
+    """An element whose gradient and moments are 0 stays where it is"""
+    for bits in (8, 32):
+        t = adam_tensors(gen(1), [300], "f32", "f32", bits, False, True)[0]
+        t["grad"].zero_()
+        keep = t["param"].clone()
+        B.smile_adamw(B.AdamW([t], beta1=0.9, beta2=0.99, eps=eps), torch.full((1,), 1e-2, device=DEV), ints(1))
+        assert torch.equal(t["param"], keep)

@@ -259,3 +259,13 @@ def test_reference_gradients_against_differences():
             ww = p.gather(1, idx.long())
             return float((dweight.double() * (ww / ww.sum(1, keepdim=True) if normalize else ww)).sum() + 0.1 * (count.double() * p.sum(0)).sum())
         assert abs((loss(1e-6) - loss(-1e-6)) / 2e-6 - float((grad * v).sum())) < 1e-6
+
+
+def test_adamw_refuses_an_eps_below_the_normal_range():
+    """fp32 has no reciprocal of it"""
+    for eps in (1e-300, 2.0 ** -149, 2.9e-39, 2.0 ** -126 * (1 - 2.0 ** -20), -1e-8, float("nan")):
+        with pytest.raises(B.SmileError) as e:
+            B.AdamW([adam()], eps=eps)
+        assert e.value.status == B.BAD_SHAPE, eps
+    for eps in (2.0 ** -126, 1e-30, 1.0):
+        B.AdamW([adam()], eps=eps)
