@@ -37,14 +37,14 @@ bool overlap(Span a, Span b)
     const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
     return p && q && p < q + b.bytes && q < p + a.bytes;
 }
-// one of what is written overlaps another, or what is read (`same`: but for the first one written, which may be exactly that)
-bool overlapping(std::initializer_list<Span> written, std::initializer_list<Span> read, const void *same = nullptr)
+// one of what is written overlaps another, or what is read (`in_place`: the first one written may be the first one read)
+bool overlapping(std::initializer_list<Span> written, std::initializer_list<Span> read, bool in_place = false)
 {
     for (auto w = written.begin(); w != written.end(); ++w) {
         for (auto o = w + 1; o != written.end(); ++o)
             if (overlap(*w, *o)) return true;
         for (const Span &r : read)
-            if (overlap(*w, r) && !(w == written.begin() && same && w->at == same && r.at == same)) return true;
+            if (overlap(*w, r) && !(in_place && w == written.begin() && &r == read.begin() && w->at == r.at)) return true;
     }
     return false;
 }
@@ -169,7 +169,7 @@ smile_status smile_topk_backward(int32_t T, int32_t N, int32_t k, int32_t normal
     const smile_status st = check_choices(T, N, k);
     if (st != SMILE_OK) return st;
     const double all = (double)T * N, pairs = (double)T * k;
-    if (overlapping({words(dlogits, all)}, {words(logits, all), words(bias, N), words(idx, pairs), words(dweight, pairs), words(count, N)}, logits)) return SMILE_INVALID_ARG;
+    if (overlapping({words(dlogits, all)}, {words(logits, all), words(bias, N), words(idx, pairs), words(dweight, pairs), words(count, N)}, true)) return SMILE_INVALID_ARG;
     return from_hip(launch_topk_backward(TopkGradIo{logits, bias, idx, dweight, count, coef, dlogits, T, N, k, normalize != 0},
                                          static_cast<hipStream_t>(stream)));
 }
@@ -213,7 +213,7 @@ smile_status smile_sorted_combine(int32_t T, int32_t k, int32_t d, int32_t R, in
     const smile_status st = check_rows(T, k, d, R, dtype);
     if (st != SMILE_OK) return st;
     const size_t row = (size_t)d * elem_size(dtype), pairs = (size_t)T * k;
-    if (overlapping({{y, T * row}}, {{residual, T * row}, {ys, R * row}, words(pos, pairs), words(weight, pairs)}, residual)) return SMILE_INVALID_ARG;
+    if (overlapping({{y, T * row}}, {{residual, T * row}, {ys, R * row}, words(pos, pairs), words(weight, pairs)}, true)) return SMILE_INVALID_ARG;
     return from_hip(launch_sorted_combine(dtype, SortedRowsIo{ys, nullptr, pos, weight, residual, y, nullptr, T, k, d, R}, static_cast<hipStream_t>(stream)));
 }
 
@@ -236,7 +236,7 @@ smile_status smile_linear(const smile_linear_args *p, void *stream)
     const smile_status st = check_linear(a.N, a.rows, a.K, a.F, a.dtype, a.act, a.start);
     if (st != SMILE_OK) return st;
     const size_t es = elem_size(a.dtype), out = (size_t)a.rows * a.F * es, bias = (size_t)a.N * a.F * es;
-    if (overlapping({{a.y, out}, {a.pre, out}}, {{a.residual, out}, {a.x, (size_t)a.rows * a.K * es}, {a.w, bias * a.K}, {a.bias, bias}, words(a.start, a.N + 1.0)}, a.residual))
+    if (overlapping({{a.y, out}, {a.pre, out}}, {{a.residual, out}, {a.x, (size_t)a.rows * a.K * es}, {a.w, bias * a.K}, {a.bias, bias}, words(a.start, a.N + 1.0)}, true))
         return SMILE_INVALID_ARG;
     return from_hip(launch_linear(a, device_tuning(), static_cast<hipStream_t>(stream)));
 }

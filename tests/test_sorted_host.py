@@ -269,3 +269,22 @@ def test_adamw_refuses_an_eps_below_the_normal_range():
         assert e.value.status == B.BAD_SHAPE, eps
     for eps in (2.0 ** -126, 1e-30, 1.0):
         B.AdamW([adam()], eps=eps)
+
+
+def test_memory_that_may_be_another_tensors_is_no_other():
+    """y may be the residual, dlogits the logits; no further tensor may lie there too, though it begins at the same place"""
+    lib = B.load()
+    M = 1 << 20
+    a = B.LinearArgs(1, 32, 64, 64, 1, 1)
+    for name, at in dict(x=M, w=2 * M, residual=M, y=M).items():
+        setattr(a, name, at)
+    assert lib.smile_linear(C.byref(a), None) == B.INVALID_ARG                    # x
+    a.x, a.bias = 3 * M, M
+    assert lib.smile_linear(C.byref(a), None) == B.INVALID_ARG                    # the bias
+    a.bias, a.w = None, M
+    assert lib.smile_linear(C.byref(a), None) == B.INVALID_ARG                    # w
+    combine = lambda ys, pos, weight: lib.smile_sorted_combine(16, 2, 64, 32, 1, ys, pos, weight, 5 * M, 5 * M, None)       # noqa: E731
+    assert combine(5 * M, 2 * M, 3 * M) == combine(M, 5 * M, 3 * M) == combine(M, 2 * M, 5 * M) == B.INVALID_ARG
+    back = lambda bias, idx, dweight, count: lib.smile_topk_backward(16, 8, 2, 1, M, bias, idx, dweight, count, 1.0, M, None)      # noqa: E731
+    for i in range(4):
+        assert back(*(M if j == i else (j + 2) * M for j in range(4))) == B.INVALID_ARG, i
