@@ -110,7 +110,7 @@ smile_status check_adamw_tensors(const smile_adamw_args &a, const smile_adamw_te
     return SMILE_OK;
 }
 
-// What a step writes, tensor by tensor: nothing of it may be there twice, or its steps would race
+// What a step writes, tensor by tensor: nothing of it may be there twice, and no gradient among it, or its chunks would race
 smile_status check_adamw_apart(const smile_adamw_args &a, const smile_adamw_tensor *tensors)
 {
     const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)a.tensors * 6]);
@@ -125,6 +125,13 @@ smile_status check_adamw_apart(const smile_adamw_args &a, const smile_adamw_tens
     std::sort(spans.get(), end, [](const Span &p, const Span &q) { return p.at < q.at; });
     for (const Span *w = spans.get(); w + 1 < end; ++w)
         if (overlap(w[0], w[1])) return SMILE_INVALID_ARG;
+    for (int i = 0; i < a.tensors; ++i) {
+        // of what lies in order and apart, the last that begins in front of the gradient's end
+        const Span grad{tensors[i].grad, (size_t)tensors[i].n * elem_size(a.grad_dtype)};
+        const void *behind = static_cast<const char *>(grad.at) + grad.bytes;
+        const Span *w = std::lower_bound(spans.get(), end, behind, [](const Span &p, const void *at) { return p.at < at; });
+        if (w != spans.get() && overlap(w[-1], grad)) return SMILE_INVALID_ARG;
+    }
     return SMILE_OK;
 }
 

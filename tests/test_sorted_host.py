@@ -288,3 +288,27 @@ def test_memory_that_may_be_another_tensors_is_no_other():
     back = lambda bias, idx, dweight, count: lib.smile_topk_backward(16, 8, 2, 1, M, bias, idx, dweight, count, 1.0, M, None)      # noqa: E731
     for i in range(4):
         assert back(*(M if j == i else (j + 2) * M for j in range(4))) == B.INVALID_ARG, i
+
+
+def test_gradients_lie_apart_from_what_a_step_writes():
+    """A chunk's gradient is read while others are stored: it shares no memory with any tensor's parameter or state.  Gradients may share theirs."""
+    flat = torch.zeros(1 << 14)
+    cut = lambda lo, n=300: flat[lo:lo + n]                                                 # noqa: E731
+    one = lambda at: dict(param=cut(at), grad=cut(at + 400), m=cut(at + 800), v=cut(at + 1200))    # noqa: E731
+    B.AdamW([one(0), one(2000), one(4000)])
+    B.AdamW([one(0), {**one(2000), "grad": cut(404)}, {**one(4000), "grad": cut(500)}])     # (between two tensors that are written)
+    for at in (0, 2000, 2296, 1704, 800, 1200, 2800 + 296, 3200 - 296):
+        for i in (0, 1):
+            tensors = [one(0), one(2000)]
+            tensors[i]["grad"] = cut(at)
+            with pytest.raises(B.SmileError) as e:
+                B.AdamW(tensors)
+            assert e.value.status == B.INVALID_ARG, (at, i)
+    for name in ("master", "m", "v", "m_scale", "v_scale"):                                 # states in 8 bits, a master
+        t = adam(n=1024, grad=torch.float32)
+        big = torch.zeros(1 << 13, dtype=torch.uint8)
+        t["grad"] = big[:4096].view(torch.float32)
+        t[name] = big[4096 - 16:4096 - 16 + t[name].numel() * t[name].element_size()].view(t[name].dtype)
+        with pytest.raises(B.SmileError) as e:
+            B.AdamW([t])
+        assert e.value.status == B.INVALID_ARG, name
