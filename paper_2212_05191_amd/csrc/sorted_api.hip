@@ -27,7 +27,7 @@ bool bad_workspace(const void *p, size_t bytes, size_t needed)
     return needed != 0 && ((reinterpret_cast<uintptr_t>(p) & 255u) != 0 || bytes < needed);
 }
 
-// memory of a call: NULL overlaps nothing
+// memory of a call: NULL overlaps nothing, nor do no bytes
 struct Span {
     const void *at;
     size_t bytes;
@@ -35,7 +35,7 @@ struct Span {
 bool overlap(Span a, Span b)
 {
     const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
-    return p && q && p < q + b.bytes && q < p + a.bytes;
+    return p && q && a.bytes && b.bytes && p < q + b.bytes && q < p + a.bytes;
 }
 // one of what is written overlaps another, or what is read (`in_place`: the first one written may be the first one read)
 bool overlapping(std::initializer_list<Span> written, std::initializer_list<Span> read, bool in_place = false)
@@ -164,7 +164,7 @@ smile_status smile_topk(int32_t T, int32_t N, int32_t k, int32_t normalize, cons
     if (needed && !workspace) return SMILE_INVALID_ARG;
     if (bad_workspace(workspace, workspace_bytes, needed)) return SMILE_WORKSPACE;
     const double pairs = (double)T * k;
-    if (overlapping({words(idx, pairs), words(weight, pairs), words(p_sum, N)}, {words(logits, (double)T * N), words(bias, N)})) return SMILE_INVALID_ARG;
+    if (overlapping({words(idx, pairs), words(weight, pairs), words(p_sum, N), {workspace, needed}}, {words(logits, (double)T * N), words(bias, N)})) return SMILE_INVALID_ARG;
     return from_hip(launch_topk(TopkIo{logits, bias, idx, weight, p_sum, static_cast<float *>(workspace), T, N, k, normalize != 0},
                                 static_cast<hipStream_t>(stream)));
 }
@@ -199,7 +199,7 @@ smile_status smile_sort_experts(int32_t T, int32_t k, int32_t N, const int32_t *
     if (needed && !workspace) return SMILE_INVALID_ARG;
     if (bad_workspace(workspace, workspace_bytes, needed)) return SMILE_WORKSPACE;
     const double pairs = (double)T * k;
-    if (overlapping({words(count, N), words(start, N + 1.0), words(pos, pairs), words(source, pairs)}, {words(idx, pairs)})) return SMILE_INVALID_ARG;
+    if (overlapping({words(count, N), words(start, N + 1.0), words(pos, pairs), words(source, pairs), {workspace, needed}}, {words(idx, pairs)})) return SMILE_INVALID_ARG;
     return from_hip(launch_sort_experts(SortIo{idx, count, start, pos, source, static_cast<int32_t *>(workspace), T * k, N}, static_cast<hipStream_t>(stream)));
 }
 
@@ -266,7 +266,7 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
     if (bad_workspace(workspace, workspace_bytes, needed)) return SMILE_WORKSPACE;
     const smile_linear_backward_args &a = *args;
     const size_t es = elem_size(a.dtype), in = (size_t)a.rows * a.K * es, out = (size_t)a.rows * a.F * es, bias = (size_t)a.N * a.F * es;
-    if (overlapping({{a.dx, in}, {a.dw, bias * a.K}, {a.dbias, bias}},
+    if (overlapping({{a.dx, in}, {a.dw, bias * a.K}, {a.dbias, bias}, {workspace, needed}},
                     {{a.dy, out}, {a.dw ? a.x : nullptr, in}, {a.dx ? a.w : nullptr, bias * a.K}, {a.act != SMILE_ACT_NONE ? a.pre : nullptr, out}, words(a.start, a.N + 1.0)}))
         return SMILE_INVALID_ARG;
     return from_hip(launch_linear_backward(*args, device_tuning(), workspace, static_cast<hipStream_t>(stream)));

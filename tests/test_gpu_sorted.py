@@ -792,3 +792,12 @@ def test_adamw_of_the_least_eps(eps):
         keep = t["param"].clone()
         B.smile_adamw(B.AdamW([t], beta1=0.9, beta2=0.99, eps=eps), torch.full((1,), 1e-2, device=DEV), ints(1))
         assert torch.equal(t["param"], keep)
+
+
+def test_a_workspace_that_is_not_needed_may_be_anything():
+    logits = normal(gen(1), 3, 8)
+    want = run_topk(logits, 2)
+    assert B.smile_topk_workspace_bytes(3, 8) == 0
+    out = [torch.zeros_like(t) for t in want]
+    B.smile_topk(logits, out[0], out[1], p_sum=out[2], workspace=logits.view(-1)[4:])
+    assert all(torch.equal(a, b) for a, b in zip(want, out))

@@ -312,3 +312,31 @@ def test_gradients_lie_apart_from_what_a_step_writes():
         with pytest.raises(B.SmileError) as e:
             B.AdamW([t])
         assert e.value.status == B.INVALID_ARG, name
+
+
+def test_workspaces_lie_apart_from_the_tensors():
+    """Kernels of one call write the workspace and read it again between reading and writing the others"""
+    lib = B.load()
+    M = 1 << 24
+    T, k, N = 20000, 2, 64
+    topk = lambda ws, **kw: lib.smile_topk(T, N, k, 1, *({**dict(logits=M, bias=2 * M, idx=3 * M, weight=4 * M, p_sum=5 * M), **kw}).values(), ws, BIG, None)       # noqa: E731
+    need = B.smile_topk_workspace_bytes(T, N)
+    assert need > 0
+    for i in range(1, 6):
+        assert topk(i * M) == B.INVALID_ARG and topk(i * M - need + 256) == B.INVALID_ARG, i
+    sort = lambda ws: lib.smile_sort_experts(T, k, N, M, 2 * M, 3 * M, 4 * M, 5 * M, ws, BIG, None)         # noqa: E731
+    need = B.smile_sort_experts_workspace_bytes(T, k, N)
+    assert need > 0
+    for i in range(1, 6):
+        assert sort(i * M) == B.INVALID_ARG and sort(i * M - need + 256) == B.INVALID_ARG, i
+    for act in (1, 2):
+        a = B.LinearBackwardArgs(2, 64, 64, 128, 1, act)
+        names = [name for name, _ in B.LinearBackwardArgs._fields_[6:]]
+        for i, name in enumerate(names):
+            setattr(a, name, (i + 1) * M)
+        size = C.c_size_t(0)
+        assert lib.smile_linear_backward_workspace_bytes(C.byref(a), C.byref(size)) == B.OK and size.value > 0
+        for i, name in enumerate(names):
+            if not (name == "pre" and act == 2):        # (not read without an activation)
+                assert lib.smile_linear_backward(C.byref(a), (i + 1) * M, BIG, None) == B.INVALID_ARG, name
+                assert lib.smile_linear_backward(C.byref(a), (i + 1) * M - size.value + 256, BIG, None) == B.INVALID_ARG, name
