@@ -321,6 +321,8 @@ smile_status smile_adamw_unpack_states(int64_t n, int32_t dtype, const void *m, 
     if (bad(m) || !m_scale || bad(v) || !v_scale || bad(m_value) || bad(v_value)) return SMILE_INVALID_ARG;
     if (dtype != SMILE_DTYPE_F32 && dtype != SMILE_DTYPE_BF16) return SMILE_UNSUPPORTED;
     if (n < 128 || n % 128 || (double)n >= kMostElements) return SMILE_BAD_SHAPE;
+    const size_t codes = (size_t)n, values = codes * elem_size(dtype);
+    if (overlapping({{m_value, values}, {v_value, values}}, {{m, codes}, {m_scale, codes / 128}, {v, codes}, {v_scale, codes / 128}})) return SMILE_INVALID_ARG;
     return from_hip(launch_adamw_unpack(dtype, n, static_cast<const uint8_t *>(m), static_cast<const uint8_t *>(m_scale), static_cast<const uint8_t *>(v),
                                         static_cast<const uint8_t *>(v_scale), m_value, v_value, static_cast<hipStream_t>(stream)));
 }

@@ -340,3 +340,14 @@ def test_workspaces_lie_apart_from_the_tensors():
             if not (name == "pre" and act == 2):        # (not read without an activation)
                 assert lib.smile_linear_backward(C.byref(a), (i + 1) * M, BIG, None) == B.INVALID_ARG, name
                 assert lib.smile_linear_backward(C.byref(a), (i + 1) * M - size.value + 256, BIG, None) == B.INVALID_ARG, name
+
+
+def test_states_as_values_lie_apart_from_their_codes():
+    lib = B.load()
+    M, n = 1 << 20, 1 << 12
+    unpack = lambda dtype=0, **kw: lib.smile_adamw_unpack_states(n, dtype, *({**dict(m=M, ms=2 * M, v=3 * M, vs=4 * M, mv=5 * M, vv=6 * M), **kw}).values(), None)    # noqa: E731
+    for wrong in (dict(mv=M), dict(vv=3 * M), dict(mv=3 * M + n - 16), dict(vv=M), dict(ms=5 * M + 1), dict(vs=6 * M + 4 * n - 1), dict(mv=6 * M), dict(mv=6 * M - 4 * n + 16),
+                  dict(m=6 * M + 4 * n - 16)):
+        assert unpack(**wrong) == B.INVALID_ARG, wrong
+    for wrong in (dict(mv=6 * M - 2 * n + 16), dict(v=5 * M + 2 * n - 16)):
+        assert unpack(dtype=1, **wrong) == B.INVALID_ARG, wrong
