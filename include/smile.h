@@ -593,7 +593,8 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
  * element's update 0.  What is not finite does not count for the block's power of two.
  * A state that decayed below fp32's normal range is kept as far as the codes reach.
  * The tensors of a plan share their types; each pointer is 16-byte aligned, the scales' excepted.  The plan is built on the host and copied to the device by the
- * caller (no tensor or state twice in it, and no gradient among them; the device copy 256-byte aligned; the step keeps a counter in it, so steps of one plan must not overlap). */
+ * caller (no tensor or state twice in it, and no gradient among them; the device copy 256-byte aligned; the step keeps a counter in it, so steps of one plan must not overlap, and
+ * lr and step are not of the plan's tensors, which the call itself does not know). */
 typedef struct smile_adamw_tensor {
     void *param;                 /* [n] in `dtype` */
     const void *grad;            /* [n] in `grad_dtype` */

@@ -311,7 +311,9 @@ smile_status smile_adamw(const smile_adamw_args *args, void *device_plan, size_t
     const smile_status st = check_adamw(*args);
     if (st != SMILE_OK) return st;
     if (args->chunks < args->tensors || args->chunks > 1ll << 40) return SMILE_BAD_SHAPE;
-    if (bad_workspace(device_plan, plan_bytes, adamw_plan_bytes(args->tensors, args->chunks))) return SMILE_WORKSPACE;
+    const size_t needed = adamw_plan_bytes(args->tensors, args->chunks);
+    if (bad_workspace(device_plan, plan_bytes, needed)) return SMILE_WORKSPACE;
+    if (overlapping({words(step, 1), {device_plan, needed}}, {words(lr, 1)})) return SMILE_INVALID_ARG;
     return from_hip(launch_adamw(*args, device_plan, lr, step, device_tuning(), static_cast<hipStream_t>(stream)));
 }
 

@@ -351,3 +351,12 @@ def test_states_as_values_lie_apart_from_their_codes():
         assert unpack(**wrong) == B.INVALID_ARG, wrong
     for wrong in (dict(mv=6 * M - 2 * n + 16), dict(v=5 * M + 2 * n - 16)):
         assert unpack(dtype=1, **wrong) == B.INVALID_ARG, wrong
+
+
+def test_step_learning_rate_and_plan_lie_apart():
+    lib = B.load()
+    M, opt = 1 << 20, B.AdamW([adam()])
+    n = opt.plan.numel()
+    call = lambda plan=M, lr=2 * M, step=3 * M: lib.smile_adamw(C.byref(opt.args), plan, n, lr, step, None)      # noqa: E731
+    for wrong in (dict(lr=3 * M), dict(lr=M), dict(lr=M + 4 * (n // 4) - 4), dict(step=M), dict(step=M + 256)):
+        assert call(**wrong) == B.INVALID_ARG, wrong
