@@ -19,7 +19,8 @@ from . import binding as B
 class SortedBlock:
     """w_router[N, d], w1[N, F, d], b1[N, F], w2[N, d, F], b2[N, d] in one storage type, for T tokens and k experts each.  The parameters are used, and updated by step(), in
     place.  normalize: weights that add up to one; balance: alpha of the load-balancing term alpha N sum_e f_e P_e; bias[N] float32 (or None) is added to the logits, -inf
-    shuts an expert off.  optimizer: bits of AdamW's states (32 or 8), or None."""
+    shuts an expert off.  optimizer: bits of AdamW's states (32 or 8), or None.  16-bit parameters have 32-bit masters, from which step() writes them: whoever loads others (a
+    checkpoint) calls take_parameters() afterwards, or the next step undoes it."""
 
     def __init__(self, T, k, w_router, w1, b1, w2, b2, act="gelu", normalize=True, bias=None, balance=0.01, training=True, optimizer=None, weight_decay=0.1, seed=0):
         N, F, d = w1.shape
@@ -105,6 +106,19 @@ class SortedBlock:
         """An AdamW step with the gradients of the last backward pass; lr[1] float32 on the device."""
         for opt, _, count in self.optimizers:
             B.smile_adamw(opt, lr, count, stream)
+
+    def take_parameters(self, new_states=False):
+        """The masters from the parameters as they are now; new_states: moments and the count of steps from zero too, as at construction."""
+        for _, tensors, count in self.optimizers:
+            for t in tensors:
+                if t["master"] is not None:
+                    t["master"].copy_(t["param"])
+                if new_states:
+                    for name in ("m", "v", "m_scale", "v_scale"):
+                        if name in t:
+                            t[name].zero_()
+            if new_states:
+                count.zero_()
 
     def close(self):
         torch.cuda.synchronize()
