@@ -240,7 +240,7 @@ template <int L, int V>
 __global__ __launch_bounds__(kThreads, V <= 8 ? 8 : V == 16 ? 5 : V == 32 ? 2 : 1) void topk_backward_kernel(TopkGradIo io)
 {
     const int lane = threadIdx.x % L;
-    const long long id = (long long)blockIdx.x * (kThreads / L) + threadIdx.x / L;
+    const long long id = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / L) + threadIdx.x / L;
     if (id >= io.T) return;
     const int t = (int)id;
     float v[V], p[V], u[V];
@@ -387,7 +387,8 @@ hipError_t launch_topk_backward(const TopkGradIo &io, hipStream_t s)
 {
     with_shape(io.T, io.N, [&](auto l, auto v) {
         const int tpb = kThreads / decltype(l)::value;
-        SMILE_LAUNCH((topk_backward_kernel<decltype(l)::value, decltype(v)::value>), dim3((io.T + tpb - 1) / tpb), dim3(kThreads), 0, s, io);
+        const int blocks = (io.T + tpb - 1) / tpb, wide = std::min(blocks, 1 << 20);   // (less than 2^32 threads a dimension)
+        SMILE_LAUNCH((topk_backward_kernel<decltype(l)::value, decltype(v)::value>), dim3(wide, (blocks + wide - 1) / wide), dim3(kThreads), 0, s, io);
         return 0;
     });
     return hipGetLastError();

@@ -144,3 +144,22 @@ def test_adamw_of_a_long_tensor():
         tol = float(lr) * (update.abs() * 20 * R.E32 + 0.1 * p0.abs() * 4 * R.E32) + 4 * R.E32 * (p0.abs() + float(lr) * update.abs())
         near(t["param"][part], want, tol * (1 + R.HALF[BF16]) + R.half_step(want, BF16) * (1 + 1e-3), "param")
     assert bool((small["m"] > 0).all()) and int(step) == 1
+
+
+def test_gradient_of_the_most_tokens():
+    """As many tokens as a call takes, one workgroup for four of them: 2^32 threads"""
+    g = gen(6)
+    T, N = 2 ** 26 - 1, 513
+    logits = torch.zeros(T, N, device=DEV)
+    at = sample(T, N)
+    logits[at] = normal(g, len(at), N, std=3.0)
+    want_idx, want_w, p, v = R.topk(logits[at], None, 1, False)
+    idx, dweight = ints(T, 1), torch.zeros(T, 1, device=DEV)
+    idx[at], dweight[at] = want_idx, normal(g, len(at), 1)
+    B.smile_topk_backward(logits, idx, dweight, logits)
+    span = (v.abs().amax(1, keepdim=True).double() * 2 + N + 16) * R.E32 * 2
+    want, terms = R.topk_backward(p, want_idx, want_w, dweight[at], False, None, 0.0)
+    size = torch.zeros_like(p).scatter_add(1, want_idx.long(), dweight[at].double().abs())
+    near(logits[at], want, p * (size + (p * size).sum(1, keepdim=True)) * (3 * span + (N + 8) * R.E32) + terms * (N + 8) * 2.0 ** -53 + 1e-36, "dlogits")
+    logits[at] = 0
+    assert not any(bool(part.any()) for part in logits.split(1 << 20))        # (tokens whose weights have no gradient)
