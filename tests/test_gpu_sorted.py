@@ -801,3 +801,38 @@ def test_a_workspace_that_is_not_needed_may_be_anything():
     out = [torch.zeros_like(t) for t in want]
     B.smile_topk(logits, out[0], out[1], p_sum=out[2], workspace=logits.view(-1)[4:])
     assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,rows,K,F,parts", [(4, 4096, 256, 256, "dw"), (4, 2000, 256, 1024, "dx"), (3, 1500, 520, 1032, "dx"), (2, 3000, 136, 2056, "dw dx"),
+                                              (7, 9000, 264, 128, "dw"), (4, 8000, 136, 4104, "dw dx")])
+def test_gradients_of_several_groups_in_parts(N, rows, K, F, parts, dtype):
+    """Sums of several groups cut into parts (the last case: tiles of 256 x 256): groups without rows, groups that end inside of a part, rows of no group in front and behind;
+    and the same bits whatever the workspace held"""
+    g = gen(rows + K)
+    cuts = [int(rows * f) for f in torch.rand(N - 1, generator=torch.Generator().manual_seed(N)).tolist()]
+    for first in ([0, *cuts, rows], [5, *cuts, rows - 37], [rows // 2] * N + [rows], [0] + [rows // 3 + 1] * (N - 1) + [rows - 1]):
+        start = torch.tensor(sorted(first), dtype=torch.int32, device=DEV)
+        x, w, b, res, y, kept, live = run_linear(g, N, rows, K, F, dtype, "gelu", True, False, start, pre=True, poison=True)
+        dy, dx, dw, db = run_linear_backward(g, x, w, kept, "gelu", start, live, dtype)
+        if dtype != "f32":
+            alone = [B.make_linear_backward_args(dy, x, w, start=start, **one) for one in (dict(dw=dw), dict(dx=dx))]
+            assert [B.smile_linear_backward_workspace_bytes(a) > 0 for a in alone] == ["dw" in parts, "dx" in parts]
+        again = [t.clone() for t in (dx, dw, db)]
+        args = B.make_linear_backward_args(dy, x, w, dx=again[0], dw=again[1], dbias=again[2], pre=kept, act="gelu", start=start)
+        B.smile_linear_backward(args, scratch(B.smile_linear_backward_workspace_bytes(args)).fill_(0xFF))
+        assert all(torch.equal(p, q) for p, q in zip((dx, dw, db), again))
+
+
+@pytest.mark.parametrize("N", (2, 6, 40))
+def test_balance_term_beside_weights_of_all_experts(N):
+    """Every expert chosen and every weight's gradient the same: the weights, which add up to one, send nothing back, and the balance term is left"""
+    g = gen(N)
+    logits, count = normal(g, 500, N, std=3.0), torch.randint(0, 50, (N,), generator=g, device=DEV, dtype=torch.int32)
+    idx, weight, _ = run_topk(logits, N, None, True)
+    d = torch.full((500, N), math.nan, device=DEV)
+    B.smile_topk_backward(logits, idx, torch.ones(500, N, device=DEV), d, normalize=True, count=count, coef=0.01)
+    p, u = torch.softmax(logits.double(), 1), 0.01 * count.double()
+    want, size = p * (u - (p * u).sum(1, keepdim=True)), p * (u + (p * u).sum(1, keepdim=True))
+    # of the weights: w (1 - sum w), where the sum of N weights is off by its N roundings, N of the sum that they were divided by and 2 of each weight
+    near(d, want, size * (2 * N + 120) * R.E32 + p * (2 * N + 6) * R.E32, "balance term")
