@@ -498,7 +498,8 @@ smile_status smile_fp8_weight_grad(int32_t N, int32_t C, int32_t Nout, int32_t K
  * Limits: T, rows, N, k, d, K, F >= 1; N <= 4096; k <= N and k <= 64; T*k < 2^26, rows and R <= 2^27; d, K, F % 8 == 0; d <= 16384,
  * K, F <= 32768; elements of any tensor below 2^40; rows * N of a product below 2^36.
  * Indices and row numbers are never followed outside their tensors: a pair whose expert is not in 0 .. N - 1 has no row, a row number that is not in
- * 0 .. R - 1 counts as none, and first rows are taken as what lies in order within 0 .. rows.
+ * 0 .. R - 1 counts as none, and a first row outside of 0 .. rows counts as its border.  First rows that are not in order lead nowhere else either, but what the products'
+ * results then hold is not defined.
  * ------------------------------------------------------------------------- */
 
 /* k experts for each of T tokens.  v[t,e] = logits[t,e] + bias[e] (one fp32 addition; bias NULL: none), -infinity where bias[e] is: such an
@@ -561,7 +562,7 @@ typedef struct smile_linear_args {
 } smile_linear_args;
 smile_status smile_linear(const smile_linear_args *args, void *stream);
 
-/* Its gradients (that of the residual is dy).  With g = dy * act'(pre), rounded to the storage type where it enters a product:
+/* Its gradients (that of the residual is dy).  With g = dy * act'(pre), rounded to the storage type where it enters a product (in half precision infinite above 65504):
  *   dx[r,:] = sum_f g[r,f] * w[e,f,:],   dw[e,f,:] = sum_r g[r,f] * x[r,:],   dbias[e,f] = sum_r g[r,f]   (g before its rounding)
  * summed in fp32 in a fixed order, rounded once.  Each of dx, dw, dbias may be NULL, but not all; w is needed for dx, x for dw, pre for
  * an activation.  Rows of no group are neither read nor written; a group without rows gets zeros. */
@@ -581,7 +582,7 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
 /* AdamW over any number of tensors in one launch, in place.  t = step[0] + 1, g the gradient, p the master weight where there is one, else the parameter:
  *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
  *   p = p - lr (weight_decay p + m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps));   param = p rounded;   step[0] = t
- * in fp32 (the powers in 64 bits).  lr[1] fp32 and step[1] int32 (>= 0) are on the device, so that a captured graph follows them.
+ * in fp32 (the powers in 64 bits; the root and the reciprocal of its sum with eps each to a unit of the last place).  lr[1] fp32 and step[1] int32 (>= 0) are on the device, so that a captured graph follows them.
  * State of 32 bits: m[n], v[n] fp32.  State of 8 bits: blocks of 128 neighbouring elements share a power of two, kept as its byte b:
  *   m: e4m3 codes times 2^(b - 127), b the least byte >= 1 for which the block's largest magnitude is at most 448 * 2^(b - 127)
  *   v: codes c of 5 exponent and 3 fraction bits without a sign, (1 + (c & 7) / 8) * 2^((c >> 3) - 30) * 2^(b - 127), 0 for c = 0; b is the power of two

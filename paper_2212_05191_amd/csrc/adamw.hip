@@ -1,9 +1,10 @@
 // AdamW over many tensors in one launch, states in 32 bits or in 8; and the values of 8-bit states.
 //
 // The tensors are cut into chunks of 2048 elements, eight a thread; a list of (tensor, chunk) made on the host lets one launch walk all of them, small
-// tensors and large.  A block of 128 elements, which shares a scale in 8-bit states, is 16 neighbouring lanes.  Bound: HBM: each element's parameter,
-// master, gradient and moments are read and written once (22 bytes an element with 8-bit states and a 32-bit master of a bfloat16 parameter: 14 of them
-// the master and the parameter, 4 the moments); everything a thread loads is requested before the first use.
+// tensors and large.  A block of 128 elements, which shares a scale in 8-bit states, is 16 neighbouring lanes.  Bound: HBM: each element's master (or
+// parameter), gradient and moments are read once, master, parameter and moments written once.  16 bytes an element with 8-bit states, a 32-bit master and a bfloat16
+// gradient: 10 of them the master and the parameter, 4 the moments, 2 the gradient; 134 M elements 472 us, 4.6 TB/s.  32-bit states: 28 bytes, 810 us, 4.6 TB/s.  Everything a
+// thread loads is requested before the first use.
 #include "fp8_device.hpp"
 #include "sorted_internal.hpp"
 
@@ -16,11 +17,13 @@ namespace {
 
 constexpr int kThreads = 256, kEach = kAdamwChunk / kThreads;
 // Workgroups on a CU, all resident: a thread has one chunk's loads in flight, so their number is what covers the memory's latency.  134 M elements with 8-bit states and
-// master weights, without and with the codes past the L2: five (88 registers) 554 / 532 us, six 514 / 490, seven (72 registers) 467, eight spill 535.
+// master weights, without and with the codes past the L2: five (88 registers) 554 / 532 us, six 514 / 490, seven (72 registers) 467 (472 since roots reach below the normal range), eight
+// spill 535.
 constexpr int kPerCu = 7;
 static_assert(kEach == 8, "eight elements a thread");
 
-// A 32-bit integer hash: xor-shifts and multiplications
+// A 32-bit integer hash: xor-shifts and multiplications.  The shifts and both multipliers are those that Chris Wellons published in 2018, found by a search for the least
+// bias: a table, so that whoever computes the bits elsewhere gets the same.
 __device__ __forceinline__ uint32_t mix(uint32_t x)
 {
     x ^= x >> 16;

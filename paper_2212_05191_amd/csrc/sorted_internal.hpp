@@ -1,5 +1,5 @@
 // Launchers of the operators of a layer without dropped tokens and of its optimizer.  Shapes were validated by the entry points
-// (sorted_api.hip, adamw_api.hip); layouts and formulas as include/smile.h says.
+// (sorted_api.hip); layouts and formulas as include/smile.h says.
 #pragma once
 
 #include "smile_internal.hpp"
