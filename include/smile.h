@@ -582,7 +582,8 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
 /* AdamW over any number of tensors in one launch, in place.  t = step[0] + 1, g the gradient, p the master weight where there is one, else the parameter:
  *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
  *   p = p - lr (weight_decay p + m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps));   param = p rounded;   step[0] = t
- * in fp32 (the powers in 64 bits; the root and the reciprocal of its sum with eps each to a unit of the last place).  lr[1] fp32 and step[1] int32 (>= 0) are on the device, so that a captured graph follows them.
+ * in fp32 (the powers in 64 bits; the root and the reciprocal of its sum with eps each to a unit of the last place).  lr[1] fp32 and
+ * step[1] int32 (>= 0) are on the device, so that a captured graph follows them.
  * State of 32 bits: m[n], v[n] fp32.  State of 8 bits: blocks of 128 neighbouring elements share a power of two, kept as its byte b:
  *   m: e4m3 codes times 2^(b - 127), b the least byte >= 1 for which the block's largest magnitude is at most 448 * 2^(b - 127)
  *   v: codes c of 5 exponent and 3 fraction bits without a sign, (1 + (c & 7) / 8) * 2^((c >> 3) - 30) * 2^(b - 127), 0 for c = 0; b is the power of two
@@ -590,8 +591,8 @@ smile_status smile_linear_backward(const smile_linear_backward_args *args, void 
  * The stored moments (not those of this step's update) are rounded up or down by 16 random bits R each: up where the part cut off is at least
  * 1 - R / 65536 of a step.  The bits are a hash of (seed, t, tensor, element), so a step gives the same bits wherever it runs.
  * m, v [n up to a multiple of 128], m_scale, v_scale [their blocks]; padding gets zero codes; all zeros is a new state.  A gradient that is not finite makes
- * its parameter and the first moment of an 8-bit state NaN.  Where it is finite and its square is not, v is infinite from then on, as the formulas have it in fp32, and the
- * element's update 0.  What is not finite does not count for the block's power of two.
+ * its parameter and the first moment of an 8-bit state NaN.  Where it is finite and its square is not, v is infinite from then on (unless beta2 is 0), as the formulas have
+ * it in fp32, and the element's update 0.  What is not finite does not count for the block's power of two.
  * A state that decayed below fp32's normal range is kept as far as the codes reach.
  * The tensors of a plan share their types; each pointer is 16-byte aligned, the scales' excepted.  The plan is built on the host and copied to the device by the
  * caller (no tensor or state twice in it, and no gradient among them; the device copy 256-byte aligned; the step keeps a counter in it, so steps of one plan must not overlap, and

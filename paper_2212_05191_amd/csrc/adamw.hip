@@ -154,7 +154,7 @@ __device__ __forceinline__ void moments(const AdamwStep &a, float g, float &m, f
 {
 #pragma clang fp contract(off)
     m = a.beta1_f * m + a.rest1 * g;
-    v = a.beta2_f * v + a.rest2 * g * g;
+    v = fmaxf(a.beta2_f * v, 0.f) + a.rest2 * g * g;   // (0 times infinity, of a v that overflowed, is NaN, and the larger of NaN and 0 is 0)
 }
 
 template <int DT, int GDT, bool EIGHT, bool MASTER>

@@ -836,3 +836,17 @@ def test_balance_term_beside_weights_of_all_experts(N):
     want, size = p * (u - (p * u).sum(1, keepdim=True)), p * (u + (p * u).sum(1, keepdim=True))
     # of the weights: w (1 - sum w), where the sum of N weights is off by its N roundings, N of the sum that they were divided by and 2 of each weight
     near(d, want, size * (2 * N + 120) * R.E32 + p * (2 * N + 6) * R.E32, "balance term")
+
+
+@pytest.mark.parametrize("bits", (8, 32))
+def test_adamw_without_a_memory_of_squares(bits):
+    """beta2 0: v is the gradient's square alone, whatever it was before, infinity included"""
+    t = adam_tensors(gen(1), [300], "f32", "f32", bits, False, True)[0]
+    opt, step = B.AdamW([t], beta1=0.0, beta2=0.0, eps=1e-30), ints(1)
+    for i, g in enumerate((1e25, 1e-3, -1e25, -2.0)):
+        before = t["param"].double().clone()
+        t["grad"][7] = g
+        B.smile_adamw(opt, torch.full((1,), 1e-2, device=DEV), step)
+        # the update is the gradient's sign (a dozen roundings), or 0 where the square is infinite
+        want = before - 1e-2 * torch.sign(t["grad"].double()) * (t["grad"].double().abs() < 1e18)
+        near(t["param"], want, 1e-2 * 16 * R.E32 + 4 * R.E32 * before.abs(), i)
